@@ -1,0 +1,498 @@
+"""Cases for measuring the 4-bit cache operators and the logit adjustment.
+
+A verify step whose paged context cache is held in 4 bits (microscaled E2M1:
+blocks of 32 consecutive head dims share a power of two) and whose logits are
+adjusted per tree node before the draw. The kinds:
+
+  attn    cascade_verify_attention_kv4: the tree's queries (or one token a
+          request) against the 4-bit context and the tree's own keys
+  append  append_kv4, then read_kv4 of what was written: a prompt into the cache
+  commit  commit_accepted_kv4, then read_kv4: accepted paths into the cache
+  read    read_kv4: a context out of the cache, as values
+  logits  adjust_logits: repetition, frequency and presence penalties, biases
+          and token masks on the logits of every tree node
+
+``own`` is false: ``run`` computes the plain form, elementary torch operations
+in 32 bits. ``own`` is true: it calls the framework's operators.
+"""
+
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda"
+D = 128          # head dim
+PAGE = 16        # tokens a page
+BLOCK = 32       # head dims that share a scale
+LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def listed():
+    return [
+        # One interactive request, one token: the latency of a decoded token.
+        dict(name="attn-bf16-b1-token-ctx4k", kind="attn", dtype="bf16", batch=1, lo=4096, hi=4096, hq=32, hkv=8, B=1, K=0),
+        # Plain decoding of a ragged batch, one token a request.
+        dict(name="attn-bf16-b64-token-ctx500-16k", kind="attn", dtype="bf16", batch=64, lo=500, hi=16000, hq=32, hkv=8, B=1, K=0),
+        # A small server: the trees of eight requests at different points of their generations.
+        dict(name="attn-bf16-b8-ctx1k-8k", kind="attn", dtype="bf16", batch=8, lo=1024, hi=8192, hq=32, hkv=8, B=16, K=4),
+        # A layer of a loaded server at 16k contexts.
+        dict(name="attn-bf16-b32-ctx16k", kind="attn", dtype="bf16", batch=32, lo=16384, hi=16384, hq=32, hkv=8, B=16, K=8),
+        # Exact-precision attention on a ragged batch.
+        dict(name="attn-f32-b4-ctx300-3k", kind="attn", dtype="f32", batch=4, lo=300, hi=3001, hq=32, hkv=8, B=16, K=4),
+        # Prompts of four requests into an empty cache.
+        dict(name="append-bf16-b4-1k-8k", kind="append", dtype="bf16", batch=4, lo=1000, hi=8191, hkv=8, ctx=0),
+        # The accepted paths of a batch into the cache.
+        dict(name="commit-f32-b32", kind="commit", dtype="f32", batch=32, hkv=8, B=16, K=4, ctx=2043),
+        # A long context back out of the cache (moved to a 16-bit cache, or to another machine).
+        dict(name="read-bf16-b2-ctx32k", kind="read", dtype="bf16", batch=2, lo=32768, hi=32768, hkv=8),
+        # A few short contexts for a check in full precision.
+        dict(name="read-f32-b5-ctx17-333", kind="read", dtype="f32", batch=5, lo=17, hi=333, hkv=2),
+        # Greedy decoding of one request with a repetition penalty only.
+        dict(name="logits-f32-b1-penalty", kind="logits", dtype="f32", batch=1, B=16, K=4, vocab=32000, hist=700, bias=0, masks=0),
+        # A loaded server: every adjustment, a token mask a node.
+        dict(name="logits-bf16-b32-all", kind="logits", dtype="bf16", batch=32, B=16, K=8, vocab=32000, hist=4000, bias=100, masks=16),
+        # Masked decoding over a large odd vocabulary.
+        dict(name="logits-bf16-b8-vocab150k", kind="logits", dtype="bf16", batch=8, B=16, K=4, vocab=150001, hist=1500, bias=20, masks=64),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _nodes(c):
+    """Most nodes of a request's tree, and how many it has in the mean."""
+    if c["B"] == 1:
+        return 1, 1.0
+    return c["B"] + c["K"] * (c["B"] - 1) - c["K"] * (c["K"] - 1) // 2, c["B"] + c["K"] * c["B"] / 2.0
+
+
+def draw(rng):
+    kind = rng.choice(["attn", "attn", "attn", "append", "commit", "read", "logits", "logits"])
+    c = dict(kind=kind, dtype=rng.choice(["bf16", "bf16", "f32"]), batch=_log_int(rng, 1, 64))
+    B = rng.choice([8, 16, 16, 24])
+    K = rng.randint(0, 6)
+    if kind == "logits":
+        c.update(B=B, K=K, vocab=rng.choice([32000, _log_int(rng, 1000, 150000), _log_int(rng, 1000, 150000) // 8 * 8]),
+                 hist=_log_int(rng, 1, 8000), bias=rng.choice([0, 1, 30, 300]), masks=rng.choice([0, 1, 40]))
+        while c["batch"] > 1 and c["batch"] * _nodes(c)[1] * c["vocab"] > 8e7:
+            c["batch"] //= 2
+        return c
+    c["hkv"] = rng.choice([1, 2, 8, 8])
+    if kind == "commit":
+        c.update(B=B, K=K, ctx=_log_int(rng, 1, 8000))
+        return c
+    hi = _log_int(rng, 1, 32768)
+    lo = hi if rng.random() < 0.3 else max(0, int(hi * rng.uniform(0.0, 1.0)))
+    while c["batch"] > 1 and c["batch"] * (hi + 16) * c["hkv"] > 6e5:
+        c["batch"] //= 2
+    c.update(lo=lo, hi=hi)
+    if kind == "append":
+        c["ctx"] = rng.choice([0, 0, _log_int(rng, 1, 3000)])
+    if kind == "attn":
+        c["hq"] = c["hkv"] * rng.choice([1, 4, 4, 5, 8])
+        c.update(B=B, K=K) if rng.random() < 0.7 else c.update(B=1, K=0)
+        most = 1.6e11 if c["dtype"] == "bf16" else 3e10
+        while c["batch"] > 1 and c["batch"] * _nodes(c)[0] * c["hq"] * (hi + 32) * 4 * D > most:
+            c["batch"] //= 2
+    return c
+
+
+# ---- inputs ----
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def _dtype(case):
+    return torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+
+
+def _lengths(case, rng):
+    """Lengths that belong to the case (every seed asks for the same work), in the seed's order."""
+    lo, hi = case["lo"], case["hi"]
+    n = np.linspace(lo, hi, case["batch"]) if case["batch"] > 1 else np.array([hi])
+    return rng.permutation(np.round(n).astype(np.int32)).astype(np.int32)
+
+
+def _parents(B, p):
+    """The block chain, then a branch per re-anchor position p under chain node p - 1."""
+    par = [-1] + list(range(B - 1))
+    for at in sorted(p):
+        par += [at - 1] + list(range(len(par), len(par) + B - at - 1))
+    return par
+
+
+def _trees(case, rng):
+    """Node offsets, parents, depths and ancestor-or-self bits of the batch's trees."""
+    B, K, W = case["B"], case["K"], (_nodes(case)[0] + 31) // 32
+    shape = np.random.default_rng(1)
+    rows = [sorted(shape.choice(np.arange(1, B), K, replace=False)) if K else [] for _ in range(case["batch"])]
+    pars = [_parents(B, [int(x) for x in rows[i]]) for i in rng.permutation(case["batch"])]
+    ip = np.concatenate([[0], np.cumsum([len(x) for x in pars])]).astype(np.int32)
+    depth, mask = np.zeros(ip[-1], np.int32), np.zeros((ip[-1], W), np.uint32)
+    for b, par in enumerate(pars):
+        for n, q in enumerate(par):
+            if q >= 0:
+                depth[ip[b] + n] = depth[ip[b] + q] + 1
+                mask[ip[b] + n] = mask[ip[b] + q]
+            mask[ip[b] + n, n // 32] |= np.uint32(1 << (n % 32))
+    return ip, pars, depth, mask.view(np.int32)
+
+
+def _cache(case, gen, pages):
+    """A 4-bit cache whose pages hold keys and values drawn from N(0, 1)."""
+    shape = (pages, case["hkv"], PAGE, D)
+    out = {}
+    for name in ("k", "v"):
+        out[name], out[name + "_scale"] = _quantise(torch.randn(shape, generator=gen, device=DEV))
+    return out
+
+
+def prepare(case, seed):
+    rng = np.random.default_rng([seed, 5])
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    kind, batch, dt = case["kind"], case["batch"], _dtype(case)
+    s = dict(kind=kind, batch=batch, dtype=dt)
+    rand = lambda *shape: torch.randn(shape, generator=gen, device=DEV).to(dt)
+    if kind in ("attn", "logits", "commit"):
+        ip, pars, depth, mask = _trees(case, rng)
+        s.update(B=case["B"], total=int(ip[-1]), max_nodes=int(np.diff(ip).max()), ip_host=ip, ip=_dev(ip),
+                 depth=_dev(depth), mask=_dev(mask), owner=_dev(np.repeat(np.arange(batch), np.diff(ip))))
+    if kind == "logits":
+        V, H, NB = case["vocab"], case["hist"], case["bias"]
+        s["logits"] = rand(s["total"], V) * 3
+        # tokens of a text come back: half of them from a small set
+        few = rng.integers(0, V, 200)
+        pick = lambda shape: np.where(rng.random(shape) < 0.5, rng.choice(few, shape), rng.integers(0, V, shape)).astype(np.int32)
+        lens = rng.permutation(np.round(np.linspace(H // 2, H, batch)).astype(np.int32)) if batch > 1 else np.array([H])
+        s.update(draft=_dev(pick(s["total"])), history=_dev(pick((batch, H))), history_len=_dev(lens.astype(np.int32)),
+                 prompt_len=_dev((lens * rng.uniform(0.2, 0.8, batch)).astype(np.int32)))
+        f = lambda lo, hi: _dev(rng.uniform(lo, hi, batch).astype(np.float32))
+        s.update(repetition=f(1.02, 1.4), presence=f(-0.5, 1.0), frequency=f(0.0, 0.6))
+        if NB:
+            tok = np.stack([rng.permutation(min(V, 4 * NB))[:NB] for _ in range(batch)]) * max(1, V // (4 * NB)) % V
+            s.update(bias_token=_dev(tok.astype(np.int32)), bias_value=_dev(rng.normal(0, 4, (batch, NB)).astype(np.float32)),
+                     bias_len=_dev(rng.integers(NB // 2, NB + 1, batch).astype(np.int32)))
+        if case["masks"]:
+            # every other mask allows few tokens, as a grammar inside a keyword does; the others most
+            words = torch.randint(-(1 << 31), 1 << 31, (3, case["masks"], (V + 31) // 32), generator=gen, device=DEV).to(torch.int32)
+            tight = (torch.arange(case["masks"], device=DEV) % 2 == 1)[:, None]
+            s["token_mask"] = torch.where(tight, words[0] & words[1] & words[2], words[0] | words[1] | words[2])
+            s["mask_row"] = _dev(rng.integers(-1, case["masks"], s["total"]).astype(np.int32))
+        return s
+    hkv = case["hkv"]
+    if kind == "commit":
+        lens, ctx = None, np.full(batch, case["ctx"], np.int32)
+        room = ctx + case["B"]
+    elif kind == "append":
+        lens, ctx = _lengths(case, rng), np.full(batch, case["ctx"], np.int32)
+        room = ctx + lens
+    else:
+        lens = ctx = room = _lengths(case, rng)
+    pages = np.maximum(1, (room + PAGE - 1) // PAGE)
+    ids, table = rng.permutation(int(pages.sum())).astype(np.int32), np.zeros((batch, int(pages.max())), np.int32)
+    for b in range(batch):
+        table[b, :pages[b]] = ids[int(pages[:b].sum()):int(pages[:b + 1].sum())]
+    s.update(_cache(case, gen, int(pages.sum())))
+    s.update(table=_dev(table), ctx=_dev(ctx), max_ctx=int(ctx.max()))
+    if kind == "commit":
+        s.update(k_new=rand(s["total"], hkv, D), v_new=rand(s["total"], hkv, D))
+        # accepted paths: the ancestors of the last node at a depth; the depths belong to the case
+        nodes = np.full((batch, case["B"]), -1, np.int32)
+        length = rng.permutation((3 * np.arange(batch) + 2) % case["B"]).astype(np.int32)
+        for b, par in enumerate(pars):
+            n = int(np.flatnonzero(depth[ip[b]:ip[b + 1]] == length[b])[-1])
+            for d in range(length[b], -1, -1):
+                nodes[b, d], n = n, par[n]
+        s.update(path_nodes=_dev(nodes), accept_len=_dev(length))
+        lens = length + 1
+    if kind != "attn":
+        tip = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+        s.update(tip=_dev(tip), tokens=int(tip[-1]), max_tokens=max(1, int(lens.max())), start=_dev(ctx if kind != "read" else 0 * ctx),
+                 token_owner=_dev(np.repeat(np.arange(batch), lens)), token_at=_dev(np.concatenate([np.arange(n) for n in lens]).astype(np.int64)))
+    if kind == "append":
+        s.update(k_new=rand(s["tokens"], hkv, D), v_new=rand(s["tokens"], hkv, D))
+    if kind == "attn":
+        s.update(q=rand(s["total"], case["hq"], D), k_tree=rand(s["total"], hkv, D), v_tree=rand(s["total"], hkv, D))
+    return s
+
+
+# ---- plain forms ----
+
+def _quantise(x):
+    """Rows of x (32 bits or fewer) in blocks of 32: packed E2M1 codes, low half first, and biased block exponents."""
+    y = x.float().reshape(*x.shape[:-1], -1, BLOCK)
+    top = y.abs().amax(-1, keepdim=True)
+    m, e = torch.frexp(top)
+    e = torch.where(top > 0, e - torch.where(m > 0.875, 2, 3), -200).clamp(-124, 125)  # smallest 2^e with top <= 7 * 2^e
+    a = torch.ldexp(y.abs(), -e)
+    code = ((a > 0.25).to(torch.uint8) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0))
+    code = (code + 8 * torch.signbit(y)).to(torch.uint8).reshape(x.shape)
+    bad = ~torch.isfinite(top)
+    return code[..., 0::2] | (code[..., 1::2] << 4), torch.where(bad, 255, e + 127).to(torch.uint8).squeeze(-1)
+
+
+def _values(packed, scale):
+    """The values that packed codes and block exponents stand for, in 32 bits."""
+    table = torch.tensor(LEVELS + tuple(-x for x in LEVELS), dtype=torch.float32, device=packed.device)
+    x = table[torch.stack([packed & 15, packed >> 4], -1).int()].reshape(*packed.shape[:-1], -1, BLOCK)
+    f = torch.where(scale == 255, math.nan, torch.exp2(scale.float() - 127))
+    return (x * f[..., None]).reshape(*packed.shape[:-1], -1)
+
+
+def _slots(s):
+    """Page and row of every new or read token."""
+    at = s["start"].long()[s["token_owner"]] + s["token_at"]
+    return s["table"].long()[s["token_owner"], at // PAGE], at % PAGE
+
+
+def _plain_write(s):
+    page, row = _slots(s)
+    at = torch.arange(s["tokens"], device=DEV)
+    if s["kind"] == "commit":
+        at = s["ip"].long()[s["token_owner"]] + s["path_nodes"].long()[s["token_owner"], s["token_at"]]
+    for name in ("k", "v"):
+        s[name][page, :, row], s[name + "_scale"][page, :, row] = _quantise(s[name + "_new"][at])
+    s["ctx"].copy_(s["start"] + s["tip"][1:] - s["tip"][:-1])
+
+
+def _plain_read(s):
+    page, row = _slots(s)
+    return {name: _values(s[name][page, :, row], s[name + "_scale"][page, :, row]).to(s["dtype"]) for name in ("k", "v")}
+
+
+def _plain_attention(s):
+    q, (total, hq, _), b, n = s["q"], s["q"].shape, s["batch"], s["max_nodes"]
+    hkv = s["k"].shape[1]
+    G = hq // hkv
+    at = s["ip"][:-1, None].long() + torch.arange(n, device=DEV)                                  # [b, n]
+    real = at < s["ip"][1:, None]
+    at = at.clamp(max=total - 1)
+    qp = q.float()[at].reshape(b, n, hkv, G, D).permute(0, 2, 1, 3, 4).reshape(b, hkv, n * G, D)
+    context = lambda x: _values(s[x], s[x + "_scale"])[s["table"].long()].permute(0, 2, 1, 3, 4).reshape(b, hkv, -1, D)
+    tree = lambda x: s[x].float()[at].permute(0, 2, 1, 3)                                         # [b, hkv, n, D]
+    C = s["table"].shape[1] * PAGE
+    keys = torch.cat([context("k"), tree("k_tree")], 2).transpose(2, 3).contiguous()
+    sc = torch.matmul(qp, keys) / math.sqrt(D)                                                    # [b, hkv, n G, C + n]
+    del keys
+    bit = torch.arange(n, device=DEV)
+    sees = ((s["mask"][at][:, :, bit // 32] >> (bit % 32)) & 1).bool() & real[:, None, :]         # [b, n, n]
+    past = torch.arange(C, device=DEV) >= s["ctx"][:, None]                                       # [b, C]
+    sc[..., :C].masked_fill_(past[:, None, None, :], -math.inf)
+    sc[..., C:].masked_fill_(~sees.repeat_interleave(G, 1)[:, None], -math.inf)
+    top = sc.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, 0.0, top)
+    p = sc.sub_(top).exp_()
+    l = p.sum(-1, keepdim=True)
+    vals = torch.cat([context("v").masked_fill_(past[:, None, :, None], 0.0), tree("v_tree")], 2).contiguous()
+    o = torch.where(l > 0, torch.matmul(p, vals) / l, 0.0).reshape(b, hkv, n, G, D).permute(0, 2, 1, 3, 4)
+    lse = (top + l.log()).reshape(b, hkv, n, G).permute(0, 2, 1, 3)
+    return {"out": o[real].reshape(total, hq, D).to(q.dtype), "lse": lse[real].reshape(total, hq)}
+
+
+def _plain_logits(s):
+    x = s["logits"].float()
+    total, V = x.shape
+    at = torch.arange(s["history"].shape[1], device=DEV)
+    there, prompt = at < s["history_len"][:, None], at < s["prompt_len"][:, None]
+    zero = torch.zeros((s["batch"], V), device=DEV)
+    new = zero.scatter_add(1, s["history"].long(), (there & ~prompt).float())                     # tokens answered so far
+    old = zero.scatter_add(1, s["history"].long(), (there & prompt).float())
+    # the draft tokens of a node's path, without the root's
+    n = torch.arange(s["max_nodes"], device=DEV)
+    first = s["ip"].long()[s["owner"]][:, None]
+    node = (first + n).clamp(max=total - 1)
+    on = ((s["mask"][:, n // 32] >> (n % 32)) & 1).bool() & (s["depth"][node] > 0)
+    count = new[s["owner"]].scatter_add_(1, s["draft"].long()[node], on.float())
+    seen = (count > 0) | (old[s["owner"]] > 0)
+    col = lambda name: s[name][s["owner"]][:, None]
+    x = torch.where(seen, torch.where(x > 0, x / col("repetition"), x * col("repetition")), x)
+    x = x - count * col("frequency") - (count > 0) * col("presence")
+    if "bias_token" in s:
+        val = s["bias_value"] * (torch.arange(s["bias_value"].shape[1], device=DEV) < s["bias_len"][:, None])
+        x = x + zero.scatter_add(1, s["bias_token"].long(), val)[s["owner"]]
+    if "token_mask" in s:
+        j = torch.arange(V, device=DEV)
+        row = s["mask_row"].long()
+        allowed = ((s["token_mask"][row.clamp(min=0)][:, j // 32] >> (j % 32)) & 1).bool() | (row < 0)[:, None]
+        x = torch.where(allowed, x, -math.inf)
+    return x.to(s["logits"].dtype)
+
+
+# ---- one pass ----
+
+def _own_pass(s):
+    from paper_2606_04446_amd import d2sd
+
+    kind = s["kind"]
+    if kind == "logits":
+        return d2sd.adjust_logits(
+            s["ip"], s["total"], s["max_nodes"], s["depth"], s["mask"], s["draft"], s["logits"], history=s["history"],
+            history_len=s["history_len"], prompt_len=s["prompt_len"], repetition=s["repetition"], presence=s["presence"],
+            frequency=s["frequency"], bias_token=s.get("bias_token"), bias_value=s.get("bias_value"), bias_len=s.get("bias_len"),
+            token_mask=s.get("token_mask"), mask_row=s.get("mask_row"))
+    if "cache" not in s:
+        s["cache"] = d2sd.Kv4Cache(s["k"], s["v"], s["k_scale"], s["v_scale"])
+    cache = s["cache"]
+    if kind == "attn":
+        if "out" not in s:  # the buffers that a serving loop keeps
+            s["out"], s["lse"] = torch.empty_like(s["q"]), torch.empty(s["q"].shape[:2], device=DEV)
+            args = d2sd.attn_args_kv4(
+                s["q"], cache, s["table"], s["ctx"], s["k_tree"], s["v_tree"], s["ip"], s["mask"], s["out"], s["lse"],
+                total_nodes=s["total"], max_nodes=s["max_nodes"], max_ctx_len=s["max_ctx"], node_indptr_host=s["ip_host"])
+            s["ws"] = torch.empty(d2sd.cascade_workspace_size_kv4(args), dtype=torch.uint8, device=DEV)
+        d2sd.cascade_verify_attention_kv4(
+            s["q"], cache, s["table"], s["ctx"], s["k_tree"], s["v_tree"], s["ip"], s["mask"], total_nodes=s["total"],
+            max_nodes=s["max_nodes"], max_ctx_len=s["max_ctx"], node_indptr_host=s["ip_host"], out=s["out"], lse=s["lse"], workspace=s["ws"])
+        return {"out": s["out"], "lse": s["lse"]}
+    if kind == "append":
+        d2sd.append_kv4(s["tip"], s["tokens"], s["max_tokens"], s["k_new"], s["v_new"], s["table"], s["ctx"], cache, s["max_ctx"])
+    if kind == "commit":
+        d2sd.commit_accepted_kv4(s["B"], s["ip"], s["total"], s["path_nodes"], s["accept_len"], s["k_new"], s["v_new"],
+                                 s["table"], s["ctx"], cache, s["max_ctx"])
+    k, v = d2sd.read_kv4(s["tip"], s["tokens"], s["max_tokens"], s["table"], cache, start=s["start"], dtype=s["dtype"])
+    return {"k": k, "v": v} if kind == "read" else {"k": k, "v": v, "ctx": s["ctx"]}
+
+
+def run(s):
+    if own:
+        return _own_pass(s)
+    if s["kind"] == "logits":
+        return _plain_logits(s)
+    if s["kind"] == "attn":
+        return _plain_attention(s)
+    if s["kind"] == "read":
+        return _plain_read(s)
+    _plain_write(s)
+    return {**_plain_read(s), "ctx": s["ctx"]}
+
+
+# ---- what a pass cannot do without ----
+
+def work(case):
+    e = 2 if case["dtype"] == "bf16" else 4
+    batch, kind = case["batch"], case["kind"]
+    if kind == "logits":
+        rows = batch * _nodes(case)[1]
+        read = rows * case["vocab"] * e + min(rows, case["masks"]) * case["vocab"] / 8 + batch * 4 * (case["hist"] * 0.75 + 2 * case["bias"])
+        return {"bytes": read + rows * case["vocab"] * e, "flops": 6.0 * rows * case["vocab"]}
+    token = case["hkv"] * (D // 2 + D // BLOCK) * 2          # bytes of a token's K and V in the cache
+    wide = case["hkv"] * D * e * 2                           # and outside of it
+    if kind == "commit":
+        tokens = batch * (1 + case["B"] / 4)
+    else:
+        tokens = batch * (case["lo"] + case["hi"]) / 2 if batch > 1 else case["hi"]
+    if kind == "read":
+        return {"bytes": tokens * (token + wide), "flops": 0.0}
+    if kind in ("append", "commit"):
+        # read, written to the cache, read from there and written as values
+        return {"bytes": tokens * (2 * wide + 2 * token), "flops": 0.0}
+    n = _nodes(case)[1]
+    qo = batch * n * case["hq"] * (D * e * 2 + 4) + batch * n * case["hkv"] * D * e * 2
+    return {"bytes": tokens * token + qo, "flops": 4.0 * D * case["hq"] * n * (tokens + batch * case["B"] / 2)}
+
+
+# ---- the same in 64 bits ----
+
+def _nearest(x):
+    """What rows in 64 bits become in 4: the nearest level times the block's power of two."""
+    y = x.reshape(*x.shape[:-1], -1, BLOCK)
+    top = y.abs().amax(-1, keepdim=True)
+    e = torch.ceil(torch.log2((top / 7).clamp(min=2.0 ** -130)))
+    e = torch.where(top > 7 * torch.exp2(e), e + 1, torch.where(top <= 7 * torch.exp2(e - 1), e - 1, e))
+    e = torch.where(top > 0, e, -124.0).clamp(-124, 125)
+    levels = torch.tensor(LEVELS, dtype=torch.float64, device=x.device)
+    a = y.abs() / torch.exp2(e)
+    off = (a[..., None] - levels).abs()
+    tie = torch.tensor([0.0, 1e-12] * 4, dtype=torch.float64, device=x.device)     # ties go to even codes
+    return (levels[(off + tie).argmin(-1)] * y.sign() * torch.exp2(e)).reshape(x.shape)
+
+
+def _held(s, name):
+    """The values of a whole cache tensor, in 64 bits."""
+    half = torch.stack([s[name] % 16, s[name] // 16], -1).long()
+    levels = torch.tensor(LEVELS, dtype=torch.float64, device=DEV)
+    x = levels[half % 8] * (1 - 2 * (half // 8))
+    x = x.reshape(*s[name].shape[:-1], D // BLOCK, BLOCK)
+    return (x * torch.exp2(s[name + "_scale"].double() - 127)[..., None]).reshape(*s[name].shape[:-1], D)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "logits":
+        return _exact_logits(case, s)
+    if kind == "attn":
+        return _exact_attention(case, s)
+    at, page = s["token_at"], None
+    if kind == "read":
+        page = s["table"].long()[s["token_owner"], at // PAGE]
+        return {n: _held(s, n)[page, :, at % PAGE] for n in ("k", "v")}
+    if kind == "commit":
+        at = s["ip"].long()[s["token_owner"]] + s["path_nodes"].long()[s["token_owner"], at]
+    else:
+        at = torch.arange(s["tokens"], device=DEV)
+    return {**{n: _nearest(s[n + "_new"][at].double()) for n in ("k", "v")}, "ctx": None}
+
+
+def _exact_attention(case, s):
+    """By definition, request by request: one softmax over the context and the ancestors-or-self."""
+    G, hkv = case["hq"] // case["hkv"], case["hkv"]
+    out = torch.zeros(s["q"].shape, dtype=torch.float64, device=DEV)
+    lse = torch.zeros(s["q"].shape[:2], dtype=torch.float64, device=DEV)
+    ctx = s["ctx"].cpu().numpy()
+    for b in range(case["batch"]):
+        i, j, C = int(s["ip_host"][b]), int(s["ip_host"][b + 1]), int(ctx[b])
+        N = j - i
+        pages = s["table"][b, :(C + PAGE - 1) // PAGE].long()
+        here = {n: s[n][pages] for n in ("k", "v", "k_scale", "v_scale")}
+        held = {n: _held(here, n).permute(1, 0, 2, 3).reshape(hkv, -1, D)[:, :C] for n in ("k", "v")}
+        word = s["mask"][i:j].cpu().numpy().view(np.uint8)
+        sees = np.unpackbits(word, axis=1, bitorder="little")[:, :N].astype(bool)
+        sees = _dev(np.concatenate([np.ones((N, C), bool), sees], 1))
+        for g in range(case["hq"]):
+            h = g // G
+            keys = torch.cat([held["k"][h], s["k_tree"][i:j, h].double()])
+            vals = torch.cat([held["v"][h], s["v_tree"][i:j, h].double()])
+            sc = (s["q"][i:j, g].double() @ keys.T.contiguous()) / math.sqrt(D)
+            sc = torch.where(sees, sc, -math.inf)
+            lse[i:j, g] = torch.logsumexp(sc, 1)
+            out[i:j, g] = torch.exp(sc - lse[i:j, g, None]) @ vals
+    return {"out": out, "lse": lse}
+
+
+def _exact_logits(case, s):
+    """By definition, node by node."""
+    host = {k: v.cpu().numpy() for k, v in s.items() if isinstance(v, torch.Tensor) and k != "logits"}
+    x = s["logits"].double()
+    V = case["vocab"]
+    for b in range(case["batch"]):
+        i, j = int(s["ip_host"][b]), int(s["ip_host"][b + 1])
+        h = host["history"][b, :host["history_len"][b]]
+        asked, said = h[:host["prompt_len"][b]], h[host["prompt_len"][b]:]
+        past = np.bincount(said, minlength=V)
+        bias = np.zeros(V)
+        if case["bias"]:
+            np.add.at(bias, host["bias_token"][b, :host["bias_len"][b]], host["bias_value"][b, :host["bias_len"][b]].astype(np.float64))
+        bias = _dev(bias)
+        r, f, o = (float(host[k][b]) for k in ("repetition", "frequency", "presence"))
+        for n in range(i, j):
+            on = np.unpackbits(host["mask"][n].view(np.uint8), bitorder="little")[:j - i].astype(bool) & (host["depth"][i:j] > 0)
+            count = past + np.bincount(host["draft"][i:j][on], minlength=V)
+            seen = count > 0
+            seen[asked] = True
+            count, seen = _dev(count.astype(np.float64)), _dev(seen)
+            y = x[n]
+            y = torch.where(seen, torch.where(y > 0, y / r, y * r), y) - f * count - o * (count > 0) + bias
+            if case["masks"] and host["mask_row"][n] >= 0:
+                word = host["token_mask"][host["mask_row"][n]]
+                y[_dev(np.unpackbits(word.view(np.uint8), bitorder="little")[:V] == 0)] = -math.inf
+            x[n] = y
+    return x
