@@ -24,6 +24,13 @@
  *   d2sd_noncascade_verify_attention
  *                         device  same attention, context re-read per tree node
  *                                 (comparison baseline)
+ *   d2sd_append_kv4, d2sd_commit_accepted_kv4, d2sd_read_kv4
+ *                         device  a paged cache in 4 bits: prompts and accepted
+ *                                 paths quantised as they are written, read back
+ *   d2sd_cascade_verify_attention_kv4
+ *                         device  the verify attention with its context in 4 bits
+ *   d2sd_adjust_logits    device  penalties for repeated tokens, biases and token
+ *                                 masks on the logits of every tree node
  *
  * Conventions (every entry point):
  *  - Ownership: the caller owns every buffer. Device pointers are device memory
@@ -482,6 +489,158 @@ d2sd_status d2sd_commit_accepted_kv(int batch, int B, int num_kv_heads, int head
                                     int total_nodes, const int* path_nodes, const int* accept_len,
                                     const void* k_tree, const void* v_tree, const int* page_table, int* ctx_len,
                                     void* k_cache, void* v_cache, hipStream_t stream);
+
+/* ------------------------------------------------------- cache in 4 bits -- */
+
+/*
+ * A paged K/V cache in 4 bits. 32 consecutive dims of a (token, KV head) row
+ * form a block that shares a power of two; an element is E2M1 (sign, 2
+ * exponent bits, 1 mantissa bit): code c & 7 stands for 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6, bit 3 is the sign. Scale byte s stands for 2^(s - 127); 255 makes all
+ * 32 values NaN. An element is worth its code's value times the scale, which
+ * is exact in bf16: 4.25 bits a value, 544 bytes instead of 2048 per 4 tokens
+ * and KV head of a 16-bit cache.
+ *   k, v             [num_pages, num_kv_heads, page_size, head_dim / 2], dim 2i
+ *                    of a row in the low half of byte i, dim 2i + 1 in the high
+ *   k_scale, v_scale [num_pages, num_kv_heads, page_size, head_dim / 32]
+ * k and v 16-byte, the scales 4-byte aligned (INVALID_ARG otherwise).
+ *
+ * How a block is written: with top the largest magnitude, the scale is the
+ * smallest 2^e >= top / 7 with -124 <= e <= 125 (e = -124 for a block of
+ * zeros); each element is the nearest E2M1 value of x / 2^e, ties to the even
+ * code, magnitudes over 6 to 6. So no element is off by more than half a step
+ * of the grid where it lies (values over 6 * 2^e: by 2^e at most) unless e
+ * is cut off at 125. A block with a NaN or an infinity gets scale byte 255.
+ */
+typedef struct d2sd_kv4_cache {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+} d2sd_kv4_cache;
+
+/*
+ * Device. Writes new tokens (a prompt, or a part of one) behind every
+ * request's context in a 4-bit cache: token t of request b goes to position
+ * ctx_len[b] + t, and ctx_len[b] grows by the request's token count.
+ *  token_indptr[batch+1]: request b's tokens are rows token_indptr[b] ..
+ *      token_indptr[b+1]-1 of k and v (none is allowed). total_tokens =
+ *      token_indptr[batch] and max_tokens, the most of a request, are host
+ *      values that bound every access.
+ *  k, v [total_tokens, num_kv_heads, head_dim] (dtype), 16-byte aligned.
+ *  page_table [batch, max_pages], ctx_len [batch] in/out: as for
+ *      d2sd_commit_accepted_kv; pages must be there for every position written.
+ *      No two requests may share a page that is written to.
+ * head_dim = D2SD_HEAD_DIM, page_size = D2SD_PAGE_SIZE, dtype D2SD_F32 or
+ * D2SD_BF16; max_ctx_len <= max_pages * page_size, which also bounds
+ * max_tokens. Tokens that would go past position max_pages * page_size - 1 are
+ * left out. Rows of the cache that are not written keep what they hold. Must
+ * not run concurrently with a call that reads the same cache or ctx_len.
+ * Errors: INVALID_ARG / UNSUPPORTED before any launch.
+ */
+d2sd_status d2sd_append_kv4(int batch, int num_kv_heads, int head_dim, int page_size, int dtype, int num_pages,
+                            int max_pages, int max_ctx_len, const int* token_indptr, int total_tokens,
+                            int max_tokens, const void* k, const void* v, const int* page_table, int* ctx_len,
+                            const d2sd_kv4_cache* cache, hipStream_t stream);
+
+/*
+ * Device. d2sd_commit_accepted_kv for a 4-bit cache: the accepted path's rows
+ * are quantised as they are written. Arguments, clamps and errors as there,
+ * with `cache` in place of k_cache and v_cache.
+ */
+d2sd_status d2sd_commit_accepted_kv4(int batch, int B, int num_kv_heads, int head_dim, int page_size, int dtype,
+                                     int num_pages, int max_pages, int max_ctx_len, const int* node_indptr,
+                                     int total_nodes, const int* path_nodes, const int* accept_len,
+                                     const void* k_tree, const void* v_tree, const int* page_table, int* ctx_len,
+                                     const d2sd_kv4_cache* cache, hipStream_t stream);
+
+/*
+ * Device. Reads a 4-bit cache back: row token_indptr[b] + t of k_out and v_out
+ * [total_tokens, num_kv_heads, head_dim] (dtype, 16-byte aligned) is the value
+ * at position start[b] + t of request b (start NULL: 0). Exact in both types
+ * (scale bytes below 2 may fall below the normal numbers of a type).
+ * token_indptr, total_tokens, max_tokens as for d2sd_append_kv4; positions
+ * outside [0, max_pages * page_size) give undefined rows.
+ */
+d2sd_status d2sd_read_kv4(int batch, int num_kv_heads, int head_dim, int page_size, int dtype, int num_pages,
+                          int max_pages, const int* token_indptr, int total_tokens, int max_tokens,
+                          const int* start, const int* page_table, const d2sd_kv4_cache* cache, void* k_out,
+                          void* v_out, hipStream_t stream);
+
+/*
+ * Host. Device workspace bytes d2sd_cascade_verify_attention_kv4 needs for
+ * `args` (0 when the contexts are not split). Errors as the call would.
+ */
+d2sd_status d2sd_cascade_workspace_size_kv4(const d2sd_attn_args* args, size_t* bytes);
+
+/*
+ * Device. d2sd_cascade_verify_attention with the context in a 4-bit cache:
+ * same queries, tree keys and values, masks, stages and outputs; the context
+ * keys and values are those that `cache` stands for. One token a request (a
+ * tree of one node) is plain decoding. args->k_cache and args->v_cache must be
+ * NULL, args->row_group and args->packed 0. kv_split as there. Products are
+ * taken with the scales applied exactly and accumulated in fp32.
+ * A tree value that is infinite or NaN reaches the rows that see its node and
+ * no other. A row that sees no key gets out = 0, lse = -inf.
+ */
+d2sd_status d2sd_cascade_verify_attention_kv4(const d2sd_attn_args* args, const d2sd_kv4_cache* cache, void* ws,
+                                              size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------ logit adjustment -- */
+
+/*
+ * Arguments of d2sd_adjust_logits. The row of tree node n of request b holds
+ * the target's logits after n; the token history that it is adjusted for is
+ * the request's own and the draft tokens on n's root path. For token j:
+ *   count = occurrences of j among history[b, prompt_len[b] .. history_len[b])
+ *           plus among the draft tokens of n and its ancestors of depth > 0
+ *           (the root's token, the anchor, belongs in the history);
+ *   seen  = count > 0 or j is among history[b, 0 .. prompt_len[b]);
+ *   x     = logits[n, j];
+ *   x     = x > 0 ? x / repetition[b] : x * repetition[b]     if seen;
+ *   x     = x - count * frequency[b] - (count > 0) * presence[b];
+ *   x     = x + the bias values of j in the request's list, in list order;
+ *   x     = -inf   if mask_row[n] >= 0 and bit j of token_mask[mask_row[n]] is 0.
+ * Evaluated in fp32 and rounded once to dtype. Lists and masks that are NULL
+ * are left out. Token ids outside [0, vocab) are ignored, lengths are clamped
+ * to the rows, mask rows >= num_masks to num_masks - 1.
+ */
+typedef struct d2sd_logits_args {
+  int batch;
+  int total_nodes;         /* host copy of node_indptr[batch] */
+  int max_nodes;           /* host upper bound of a request's nodes, in [1, 2080] */
+  int mask_words;          /* row stride of anc_mask; >= ceil(max_nodes / 32) */
+  int vocab;               /* 1 <= vocab <= D2SD_MAX_VOCAB */
+  int dtype;               /* of logits and out: D2SD_F32 or D2SD_BF16 */
+  int max_history;         /* row stride of history, >= 0 (0: no history) */
+  int max_bias;            /* row stride of bias_token and bias_value, >= 0 (0: none) */
+  int num_masks;           /* rows of token_mask, >= 0 (0: none) */
+  const int* node_indptr;  /* [batch + 1] */
+  const int* depth;        /* [total_nodes], as from d2sd_tree_build */
+  const uint32_t* anc_mask; /* [total_nodes, mask_words] */
+  const int* draft_tokens; /* [total_nodes] */
+  const void* logits;      /* [total_nodes, vocab], 16-byte aligned */
+  const int* history;      /* [batch, max_history] */
+  const int* history_len;  /* [batch] */
+  const int* prompt_len;   /* [batch]; nullable: 0 */
+  const float* repetition; /* [batch], > 0; nullable: 1 */
+  const float* presence;   /* [batch]; nullable: 0 */
+  const float* frequency;  /* [batch]; nullable: 0 */
+  const int* bias_token;   /* [batch, max_bias] */
+  const float* bias_value; /* [batch, max_bias] */
+  const int* bias_len;     /* [batch]; nullable: max_bias */
+  const uint32_t* token_mask; /* [num_masks, ceil(vocab / 32)], bit j % 32 of word j / 32 */
+  const int* mask_row;     /* [total_nodes] */
+  void* out;               /* [total_nodes, vocab], 16-byte aligned; may be logits */
+} d2sd_logits_args;
+
+/*
+ * Device. Adjusts the logits of every tree node (see d2sd_logits_args) for
+ * d2sd_sample_targets or an argmax. A row whose mask leaves nothing is all
+ * -inf, for which d2sd_sample_targets gives -1. One launch, no workspace.
+ * Errors: INVALID_ARG before any launch.
+ */
+d2sd_status d2sd_adjust_logits(const d2sd_logits_args* args, hipStream_t stream);
 
 /* ------------------------------------------------------------ profiling -- */
 

@@ -7,11 +7,16 @@
 #include <string>
 #include <vector>
 
+#include "host.h"
 #include "launchers.h"
 
 namespace {
 
 thread_local std::string g_last_error;
+
+}  // namespace
+
+namespace d2sd {
 
 d2sd_status fail(d2sd_status s, const char* fmt, ...) {
   char buf[512];
@@ -32,6 +37,16 @@ d2sd_status hip_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return ok();
   return fail(D2SD_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace d2sd
+
+namespace {
+
+using d2sd::fail;
+using d2sd::hip_status;
+using d2sd::ok;
+using d2sd::kMaxTreeNodes;
+using d2sd::validate_attn;
 
 // ---- kernel timing (HIP events around the context-streaming kernel) ----
 std::mutex g_timing_mu;
@@ -109,10 +124,6 @@ hipError_t collect_timings(std::vector<float>* kernel, std::vector<float>* merge
   return err;
 }
 
-// Largest tree any entry point accepts: the canonical tree of B = D2SD_MAX_B
-// with every re-anchor position (the accept kernel stages one tree in LDS).
-constexpr int kMaxTreeNodes = D2SD_MAX_B + D2SD_MAX_B * (D2SD_MAX_B - 1) / 2;
-
 int mask_words_for(int B) {
   if (B < 2 || B > D2SD_MAX_B) return 0;
   return (B + B * (B - 1) / 2 + 31) / 32;
@@ -125,7 +136,11 @@ constexpr int kMinSplit = 256;      // bf16: shorter splits cost more in partial
 constexpr int kMinSplitF32 = 64;    // fp32: a split is compute-bound (fp32 MFMA), parallelism pays
 constexpr int kMaxSplit = 32768;   // the bf16 kernel stages a split's page ids in LDS
 
-d2sd_status validate_attn(const d2sd_attn_args* a, bool need_ws_fields) {
+}  // namespace
+
+namespace d2sd {
+
+d2sd_status validate_attn(const d2sd_attn_args* a, bool pointers) {
   if (!a) return fail(D2SD_ERR_INVALID_ARG, "args is NULL");
   if (a->batch < 1) return fail(D2SD_ERR_INVALID_ARG, "batch must be >= 1 (got %d)", a->batch);
   if (a->num_qo_heads < 1 || a->num_kv_heads < 1)
@@ -177,7 +192,7 @@ d2sd_status validate_attn(const d2sd_attn_args* a, bool need_ws_fields) {
         return fail(D2SD_ERR_INVALID_ARG, "node_indptr_host: request %d has %d nodes, outside [0, max_nodes %d]",
                     b, ip[b + 1] - ip[b], a->max_nodes);
   }
-  if (!need_ws_fields) return D2SD_OK;
+  if (!pointers) return D2SD_OK;
   if (!a->q || !a->k_cache || !a->v_cache || !a->page_table || !a->ctx_len || !a->k_tree ||
       !a->v_tree || !a->node_indptr || !a->out)
     return fail(D2SD_ERR_INVALID_ARG, "a required device pointer is NULL");
@@ -191,6 +206,10 @@ d2sd_status validate_attn(const d2sd_attn_args* a, bool need_ws_fields) {
       return fail(D2SD_ERR_INVALID_ARG, "%s is not 16-byte aligned", names[i]);
   return D2SD_OK;
 }
+
+}  // namespace d2sd
+
+namespace {
 
 // Row groups (work items) of one context split over the batch, for groups of
 // rows_per_group query rows: exact when the host copy of the node offsets is

@@ -1,0 +1,262 @@
+// Logit adjustment per tree node: penalties for repeated tokens, biases and
+// token masks (definition: d2sd_logits_args in d2sd.h).
+//
+// The adjustment of token j is the same for all nodes of a request but for the
+// few draft tokens on their root paths, so it is y = x * (x > 0 ? mp : mn) + a
+// with mp, mn and a per (request, token). A workgroup takes a chunk of the
+// vocabulary of one request, builds these from the request's token history and
+// bias list (counted in LDS, kept in registers, 16 tokens a thread), and then
+// streams the chunk of each of its nodes' rows past them: one read and one
+// write of the logits, plus a bit per token where the node has a mask. Draft
+// tokens in the chunk are listed per owning thread; a thread with a non-empty
+// list corrects its registers for the entries that are ancestors of the node,
+// and the others never look, so the loop has no barrier. Counts are integers
+// and bias lists are summed in order, so results do not depend on timing.
+// Bound by memory: 2 bytes in and 2 out per bf16 logit.
+#include "launchers.h"
+
+namespace d2sd {
+
+namespace {
+
+constexpr int kThr = 256;
+constexpr int kElems = 16;                          // tokens per thread
+constexpr int kChunk = kThr * kElems;
+constexpr int kListMax = D2SD_MAX_B + D2SD_MAX_B * (D2SD_MAX_B - 1) / 2;   // nodes of a request
+constexpr uint32_t kNoEntry = 0xfffu;
+constexpr uint32_t kPromptBit = 1u << 31;
+static_assert(kListMax < (int)kNoEntry, "list entries are linked by 12 bits");
+
+template <typename T>
+struct Vec;
+template <>
+struct Vec<__bf16> {
+  static constexpr int N = 8;
+};
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+};
+
+// 16 bytes at an address aligned to the element only: rows of an odd
+// vocabulary start anywhere, and gfx9 global accesses take any alignment.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+struct __attribute__((packed)) Loose16 {
+  u32x4 v;
+};
+
+template <typename T>
+__device__ __forceinline__ u32x4 load_vec(const T* row, int j, int V) {
+  constexpr int N = Vec<T>::N;
+  if (j + N <= V) return reinterpret_cast<const Loose16*>(row + j)->v;
+  union {
+    T e[N];
+    u32x4 v;
+  } u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) u.e[i] = row[min(j + i, V - 1)];
+  return u.v;
+}
+template <typename T>
+__device__ __forceinline__ void store_vec(T* row, int j, int V, const u32x4& x) {
+  constexpr int N = Vec<T>::N;
+  if (j + N <= V) {
+    reinterpret_cast<Loose16*>(row + j)->v = x;
+    return;
+  }
+  union {
+    u32x4 v;
+    T e[N];
+  } u;
+  u.v = x;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (j + i < V) row[j + i] = u.e[i];
+}
+
+__device__ __forceinline__ void unpack(const u32x4& x, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(x[i] << 16);
+    v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const u32x4& x, float (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(x[i]);
+}
+__device__ __forceinline__ u32x4 pack(const float (&v)[8]) {
+  union {
+    __bf16 e[8];
+    u32x4 v;
+  } u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) u.e[i] = (__bf16)v[i];
+  return u.v;
+}
+__device__ __forceinline__ u32x4 pack(const float (&v)[4]) {
+  return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThr) void adjust_logits_kernel(d2sd_logits_args a, int chunks, int groups, int nodes_per_group) {
+  constexpr int N = Vec<T>::N;                      // tokens of a 16-byte vector
+  constexpr int kVecs = kElems / N;                 // vectors per thread: tokens v kThr N + t N .. + N of the chunk
+  __shared__ uint32_t s_tok[kChunk];                // counts, then bias values
+  __shared__ uint32_t s_list[kListMax];             // next entry << 16 | token of the thread << 12 | node
+  __shared__ uint32_t s_head[kThr];
+  __shared__ int s_n;
+
+  int rest = blockIdx.x;
+  const int ck = rest % chunks; rest /= chunks;
+  const int grp = rest % groups;
+  const int b = rest / groups;
+  const int base = clampi(a.node_indptr[b], 0, a.total_nodes);
+  const int nodes = clampi(a.node_indptr[b + 1], base, min(a.total_nodes, base + a.max_nodes)) - base;
+  const int n0 = grp * nodes_per_group, n1 = min(nodes, n0 + nodes_per_group);
+  if (n0 >= n1) return;
+  const int c0 = ck * kChunk;                       // tokens c0 .. c0 + here - 1
+  const int here = min(kChunk, a.vocab - c0);
+  const int t = threadIdx.x;
+
+  // ---- what the request's history and biases make of the chunk ----
+#pragma unroll
+  for (int i = 0; i < kElems; ++i) s_tok[i * kThr + t] = 0;
+  s_head[t] = kNoEntry;
+  if (t == 0) s_n = 0;
+  __syncthreads();
+  if (a.max_history > 0) {
+    const int* hist = a.history + (size_t)b * a.max_history;
+    const int len = clampi(a.history_len[b], 0, a.max_history);
+    const int prompt = a.prompt_len ? clampi(a.prompt_len[b], 0, len) : 0;
+    for (int i = t; i < len; i += kThr) {
+      const uint32_t off = (uint32_t)hist[i] - (uint32_t)c0;
+      if (off >= (uint32_t)here) continue;
+      if (i < prompt)
+        atomicOr(&s_tok[off], kPromptBit);
+      else
+        atomicAdd(&s_tok[off], 1u);
+    }
+  }
+  // draft tokens of the chunk, linked by the thread that owns them
+  for (int n = t; n < nodes; n += kThr) {
+    const uint32_t off = (uint32_t)a.draft_tokens[base + n] - (uint32_t)c0;
+    if (off >= (uint32_t)here || a.depth[base + n] <= 0) continue;
+    const int owner = (int)off % (kThr * N) / N;
+    const uint32_t e = (uint32_t)off / (kThr * N) * N + off % N;
+    const uint32_t at = (uint32_t)atomicAdd(&s_n, 1);
+    s_list[at] = atomicExch(&s_head[owner], at) << 16 | e << 12 | (uint32_t)n;
+  }
+  __syncthreads();
+  const float rep = a.repetition ? a.repetition[b] : 1.0f;
+  const float inv_rep = 1.0f / rep;
+  const float pres = a.presence ? a.presence[b] : 0.0f;
+  const float freq = a.frequency ? a.frequency[b] : 0.0f;
+  uint32_t seen = 0, counted = 0;                   // a bit per token of the thread
+  float add[kElems];
+#pragma unroll
+  for (int i = 0; i < kElems; ++i) {
+    const uint32_t c = s_tok[i / N * (kThr * N) + t * N + i % N];
+    const float n = (float)(c & ~kPromptBit);
+    add[i] = c & ~kPromptBit ? -(n * freq) - pres : 0.0f;
+    seen |= (c ? 1u : 0u) << i;
+    counted |= (c & ~kPromptBit ? 1u : 0u) << i;
+  }
+  if (a.max_bias > 0) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kElems; ++i) s_tok[i * kThr + t] = 0;
+    __syncthreads();
+    const int* tok = a.bias_token + (size_t)b * a.max_bias;
+    const float* val = a.bias_value + (size_t)b * a.max_bias;
+    const int len = a.bias_len ? clampi(a.bias_len[b], 0, a.max_bias) : a.max_bias;
+    for (int i = t; i < len; i += kThr) {
+      const int j = tok[i];
+      const uint32_t off = (uint32_t)j - (uint32_t)c0;
+      if (off >= (uint32_t)here) continue;
+      bool first = true;                            // the token's first entry sums them all, in order
+      for (int k = 0; k < i && first; ++k) first = tok[k] != j;
+      if (!first) continue;
+      float sum = val[i];
+      for (int k = i + 1; k < len; ++k)
+        if (tok[k] == j) sum += val[k];
+      s_tok[off] = __float_as_uint(sum);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kElems; ++i) add[i] += __uint_as_float(s_tok[i / N * (kThr * N) + t * N + i % N]);
+  }
+  const uint32_t head = s_head[t];
+
+  // ---- the rows ----
+  const T* in = static_cast<const T*>(a.logits);
+  T* out = static_cast<T*>(a.out);
+  const int words = (a.vocab + 31) >> 5;
+  for (int n = n0; n < n1; ++n) {
+    const size_t row = (size_t)(base + n) * a.vocab;
+    const int mr = a.num_masks > 0 ? min(a.mask_row[base + n], a.num_masks - 1) : -1;
+    u32x4 raw[kVecs];
+    uint32_t allowed[kVecs];
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      const int j = c0 + v * (kThr * N) + t * N;
+      allowed[v] = ~0u;
+      if (j >= a.vocab) continue;
+      raw[v] = load_vec(in + row, j, a.vocab);
+      if (mr >= 0) allowed[v] = a.token_mask[(size_t)mr * words + (j >> 5)] >> (j & 31);
+    }
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      const int j = c0 + v * (kThr * N) + t * N;
+      if (j >= a.vocab) continue;
+      float x[N];
+      unpack(raw[v], x);
+      float y[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int e = v * N + i;
+        const float f = (seen >> e) & 1u ? (x[i] > 0.0f ? inv_rep : rep) : 1.0f;
+        y[i] = x[i] * f + add[e];
+      }
+      for (uint32_t at = head; at != kNoEntry; at = s_list[at] >> 16) {
+        const uint32_t e = (s_list[at] >> 12) & 15u;
+        if ((int)e / N != v) continue;
+        // how many of the node's ancestors-or-self draft this token
+        int hits = 0;
+        for (uint32_t k = head; k != kNoEntry; k = s_list[k] >> 16) {
+          const uint32_t m = s_list[k] & 0xfffu;
+          if (((s_list[k] >> 12) & 15u) == e)
+            hits += (a.anc_mask[(size_t)(base + n) * a.mask_words + (m >> 5)] >> (m & 31)) & 1u;
+        }
+        if (hits == 0) continue;
+        const float more = -((float)hits * freq) - ((counted >> e) & 1u ? 0.0f : pres);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (v * N + i == (int)e) y[i] = x[i] * (x[i] > 0.0f ? inv_rep : rep) + (add[v * N + i] + more);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (!((allowed[v] >> i) & 1u)) y[i] = -INFINITY;
+      store_vec(out + row, j, a.vocab, pack(y));
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_adjust_logits(const d2sd_logits_args& a, hipStream_t stream) {
+  const int chunks = ceil_div(a.vocab, kChunk);
+  // Nodes per workgroup: the history is counted once for all of them, but
+  // there should be some eight workgroups for each of the 256 CUs.
+  const long long rows = (long long)a.total_nodes * chunks;
+  const int per = (int)max(1ll, min(8ll, rows / 2048));
+  const int groups = ceil_div(a.max_nodes, per);
+  const dim3 grid((unsigned)((long long)a.batch * groups * chunks));
+  if (a.dtype == D2SD_BF16)
+    hipLaunchKernelGGL(adjust_logits_kernel<__bf16>, grid, dim3(kThr), 0, stream, a, chunks, groups, per);
+  else
+    hipLaunchKernelGGL(adjust_logits_kernel<float>, grid, dim3(kThr), 0, stream, a, chunks, groups, per);
+  return hipGetLastError();
+}
+
+}  // namespace d2sd

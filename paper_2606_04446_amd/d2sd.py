@@ -63,6 +63,25 @@ class AttnArgs(ctypes.Structure):
         self._keep = getattr(self, "_keep", ()) + objs
 
 
+class Kv4Pointers(ctypes.Structure):
+    """Mirror of d2sd_kv4_cache."""
+
+    _fields_ = [("k", _c_ptr), ("v", _c_ptr), ("k_scale", _c_ptr), ("v_scale", _c_ptr)]
+
+
+class LogitsArgs(ctypes.Structure):
+    """Mirror of d2sd_logits_args (field order and types must match the header)."""
+
+    _fields_ = [
+        ("batch", _c_int), ("total_nodes", _c_int), ("max_nodes", _c_int), ("mask_words", _c_int), ("vocab", _c_int),
+        ("dtype", _c_int), ("max_history", _c_int), ("max_bias", _c_int), ("num_masks", _c_int),
+        ("node_indptr", _c_ptr), ("depth", _c_ptr), ("anc_mask", _c_ptr), ("draft_tokens", _c_ptr), ("logits", _c_ptr),
+        ("history", _c_ptr), ("history_len", _c_ptr), ("prompt_len", _c_ptr), ("repetition", _c_ptr),
+        ("presence", _c_ptr), ("frequency", _c_ptr), ("bias_token", _c_ptr), ("bias_value", _c_ptr),
+        ("bias_len", _c_ptr), ("token_mask", _c_ptr), ("mask_row", _c_ptr), ("out", _c_ptr),
+    ]
+
+
 def _sig(name, restype, *argtypes):
     f = getattr(_lib, name)
     f.restype = restype
@@ -96,6 +115,17 @@ _accept = _sig("d2sd_accept_path", _c_int, _c_int, _c_int, _c_ptr, _c_int, _c_pt
                _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr)
 _sample = _sig("d2sd_sample_targets", _c_int, _c_int, _c_ptr, _c_int, _c_int, _c_ptr, _c_ptr, _c_int, _c_int, _c_ptr,
                 ctypes.c_float, _c_ptr, _c_ptr, _c_ptr, _c_ptr)
+_kv4_p = ctypes.POINTER(Kv4Pointers)
+_append_kv4 = _sig("d2sd_append_kv4", _c_int, *[_c_int] * 8, _c_ptr, _c_int, _c_int, _c_ptr, _c_ptr, _c_ptr, _c_ptr,
+                   _kv4_p, _c_ptr)
+_commit_kv4 = _sig("d2sd_commit_accepted_kv4", _c_int, *[_c_int] * 9, _c_ptr, _c_int, _c_ptr, _c_ptr, _c_ptr, _c_ptr,
+                   _c_ptr, _c_ptr, _kv4_p, _c_ptr)
+_read_kv4 = _sig("d2sd_read_kv4", _c_int, *[_c_int] * 7, _c_ptr, _c_int, _c_int, _c_ptr, _c_ptr, _kv4_p, _c_ptr,
+                 _c_ptr, _c_ptr)
+_ws_size_kv4 = _sig("d2sd_cascade_workspace_size_kv4", _c_int, ctypes.POINTER(AttnArgs), ctypes.POINTER(_c_size))
+_cascade_kv4 = _sig("d2sd_cascade_verify_attention_kv4", _c_int, ctypes.POINTER(AttnArgs), _kv4_p, _c_ptr, _c_size,
+                    _c_ptr)
+_adjust = _sig("d2sd_adjust_logits", _c_int, ctypes.POINTER(LogitsArgs), _c_ptr)
 _timing_enable = _sig("d2sd_kernel_timing_enable", _c_int, _c_int)
 _timing_collect = _sig("d2sd_kernel_timing_collect", _c_int, _c_int_p, ctypes.POINTER(ctypes.c_double))
 _timing_each = _sig("d2sd_kernel_timing_collect_each", _c_int, _c_int, ctypes.POINTER(ctypes.c_float), _c_int_p)
@@ -445,6 +475,194 @@ def sample_targets(node_indptr, total_nodes: int, max_nodes: int, parent, draft_
                    float(temperature), _dev(uniform, "uniform", torch.float32), _dev(reps, "context_rep", i32),
                    _dev(tokens, "target_tokens", i32), _stream(stream)), "d2sd_sample_targets")
     return tokens[:total_nodes], (reps[:total_nodes] if reps is not None else None)
+
+
+# -------------------------------------------------------- cache in 4 bits --
+
+class Kv4Cache:
+    """A paged K/V cache in 4 bits (layout and rounding: d2sd_kv4_cache in the
+    header): k, v uint8 [num_pages, num_kv_heads, 16, 64], k_scale, v_scale
+    uint8 [num_pages, num_kv_heads, 16, 4], contiguous device tensors."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        if k.dim() != 4 or k.shape[2:] != (PAGE_SIZE, HEAD_DIM // 2):
+            raise ValueError(f"k must be [pages, kv heads, {PAGE_SIZE}, {HEAD_DIM // 2}], got {tuple(k.shape)}")
+        scales = (*k.shape[:3], HEAD_DIM // 32)
+        for t, name, shape in ((v, "v", k.shape), (k_scale, "k_scale", scales), (v_scale, "v_scale", scales)):
+            if tuple(t.shape) != tuple(shape):
+                raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+            if t.device != k.device:
+                raise ValueError(f"{name} must be on {k.device}, got {t.device}")
+        u8 = torch.uint8
+        self.pointers = Kv4Pointers(_dev(k, "k", u8), _dev(v, "v", u8), _dev(k_scale, "k_scale", u8),
+                                    _dev(v_scale, "v_scale", u8))
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.num_pages, self.num_kv_heads = k.shape[0], k.shape[1]
+
+    @classmethod
+    def empty(cls, num_pages: int, num_kv_heads: int, device="cuda"):
+        """A cache of zeros (codes and scale bytes 0)."""
+        z = lambda n: torch.zeros((num_pages, num_kv_heads, PAGE_SIZE, n), dtype=torch.uint8, device=device)
+        return cls(z(HEAD_DIM // 2), z(HEAD_DIM // 2), z(HEAD_DIM // 32), z(HEAD_DIM // 32))
+
+
+def _rows_code(t, name, rows, heads, dtype=None):
+    """dtype code of a [rows, heads, 128] tensor."""
+    if tuple(t.shape) != (rows, heads, HEAD_DIM):
+        raise ValueError(f"{name} must have shape ({rows}, {heads}, {HEAD_DIM}), got {tuple(t.shape)}")
+    code = {torch.float32: F32, torch.bfloat16: BF16}.get(t.dtype)
+    if code is None or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} dtype {t.dtype} unsupported (float32 or bfloat16, K and V alike)")
+    return code
+
+
+def append_kv4(token_indptr, total_tokens: int, max_tokens: int, k, v, page_table, ctx_len, cache: Kv4Cache,
+               max_ctx_len: int, stream=None):
+    """Quantise new tokens' K/V [total_tokens, kv heads, 128] (float32 or
+    bfloat16) behind every request's context and advance ctx_len (in place)."""
+    code = _rows_code(k, "k", total_tokens, cache.num_kv_heads)
+    _rows_code(v, "v", total_tokens, cache.num_kv_heads, k.dtype)
+    i32 = torch.int32
+    _check(_append_kv4(ctx_len.numel(), cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
+                       page_table.shape[1], max_ctx_len, _dev(token_indptr, "token_indptr", i32), total_tokens,
+                       max_tokens, _dev(k, "k"), _dev(v, "v"), _dev(page_table, "page_table", i32),
+                       _dev(ctx_len, "ctx_len", i32), cache.pointers, _stream(stream)), "d2sd_append_kv4")
+
+
+def commit_accepted_kv4(B: int, node_indptr, total_nodes: int, path_nodes, accept_len, k_tree, v_tree, page_table,
+                        ctx_len, cache: Kv4Cache, max_ctx_len: int, stream=None):
+    """commit_accepted_kv for a 4-bit cache: the accepted rows are quantised as
+    they are written (in place on the cache and on ctx_len)."""
+    code = _rows_code(k_tree, "k_tree", k_tree.shape[0], cache.num_kv_heads)
+    _rows_code(v_tree, "v_tree", k_tree.shape[0], cache.num_kv_heads, k_tree.dtype)
+    i32 = torch.int32
+    _check(_commit_kv4(ctx_len.numel(), B, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
+                       page_table.shape[1], max_ctx_len, _dev(node_indptr, "node_indptr", i32), total_nodes,
+                       _dev(path_nodes, "path_nodes", i32), _dev(accept_len, "accept_len", i32),
+                       _dev(k_tree, "k_tree"), _dev(v_tree, "v_tree"), _dev(page_table, "page_table", i32),
+                       _dev(ctx_len, "ctx_len", i32), cache.pointers, _stream(stream)), "d2sd_commit_accepted_kv4")
+
+
+def read_kv4(token_indptr, total_tokens: int, max_tokens: int, page_table, cache: Kv4Cache, start=None,
+             dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
+    """The values a 4-bit cache stands for: row token_indptr[b] + t is position
+    start[b] + t of request b. Returns (k, v) [total_tokens, kv heads, 128]."""
+    shape = (total_tokens, cache.num_kv_heads, HEAD_DIM)
+    k = k_out if k_out is not None else torch.empty(shape, dtype=dtype, device=cache.k.device)
+    v = v_out if v_out is not None else torch.empty(shape, dtype=k.dtype, device=cache.k.device)
+    code = _rows_code(k, "k_out", total_tokens, cache.num_kv_heads)
+    _rows_code(v, "v_out", total_tokens, cache.num_kv_heads, k.dtype)
+    i32 = torch.int32
+    _check(_read_kv4(page_table.shape[0], cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
+                     page_table.shape[1], _dev(token_indptr, "token_indptr", i32), total_tokens, max_tokens,
+                     _dev(start, "start", i32), _dev(page_table, "page_table", i32), cache.pointers, _dev(k, "k_out"),
+                     _dev(v, "v_out"), _stream(stream)), "d2sd_read_kv4")
+    return k, v
+
+
+def attn_args_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, out, lse, *,
+                  total_nodes: int, max_nodes: int, max_ctx_len: int, stage: int = STAGE_CASCADE,
+                  sm_scale: float = 0.0, kv_split: int = 0, node_indptr_host=None) -> AttnArgs:
+    """attn_args for a context in a 4-bit cache (k_cache and v_cache stay NULL)."""
+    dt = q.dtype
+    code = {torch.float32: F32, torch.bfloat16: BF16}.get(dt)
+    if code is None:
+        raise ValueError(f"q dtype {dt} unsupported (float32 or bfloat16)")
+    i32 = torch.int32
+    a = AttnArgs(ctx_len.numel(), q.shape[1], cache.num_kv_heads, q.shape[2], PAGE_SIZE, code, stage, sm_scale,
+                 total_nodes, max_nodes, max_ctx_len, cache.num_pages, page_table.shape[1],
+                 anc_mask.shape[1] if anc_mask is not None else 0, kv_split, 0, 0, _dev(q, "q", dt), None, None,
+                 _dev(page_table, "page_table", i32), _dev(ctx_len, "ctx_len", i32), _dev(k_tree, "k_tree", dt),
+                 _dev(v_tree, "v_tree", dt), _dev(node_indptr, "node_indptr", i32), _dev(anc_mask, "anc_mask", i32),
+                 _dev(out, "out", dt), _dev(lse, "lse", torch.float32), None)
+    if node_indptr_host is not None:
+        ip = _host_i32(node_indptr_host)
+        if ip.shape != (a.batch + 1,):
+            raise ValueError(f"node_indptr_host must have {a.batch + 1} entries, got {ip.shape}")
+        a.node_indptr_host = ip.__array_interface__["data"][0]
+        a.keep(ip)
+    return a
+
+
+def cascade_workspace_size_kv4(args: AttnArgs) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_ws_size_kv4(ctypes.byref(args), ctypes.byref(n)), "d2sd_cascade_workspace_size_kv4")
+    return n.value
+
+
+def cascade_verify_attention_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, *,
+                                 total_nodes: int, max_nodes: int, max_ctx_len: int, stage: int = STAGE_CASCADE,
+                                 sm_scale: float = 0.0, kv_split: int = 0, out=None, lse=None, workspace=None,
+                                 want_lse: bool = True, node_indptr_host=None, stream=None):
+    """Verify attention with the context in a 4-bit cache; returns (out, lse).
+    The workspace is allocated when not given."""
+    if out is None:
+        out = torch.empty_like(q)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    a = attn_args_kv4(q, cache, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, out, lse,
+                      total_nodes=total_nodes, max_nodes=max_nodes, max_ctx_len=max_ctx_len, stage=stage,
+                      sm_scale=sm_scale, kv_split=kv_split, node_indptr_host=node_indptr_host)
+    if workspace is None:      # a given one is checked against the call's need by the library
+        need = cascade_workspace_size_kv4(a)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    ws_ptr = _dev(workspace, "workspace") if workspace is not None else None
+    ws_len = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    _check(_cascade_kv4(ctypes.byref(a), cache.pointers, ws_ptr, ws_len, _stream(stream)),
+           "d2sd_cascade_verify_attention_kv4")
+    return out, lse
+
+
+# ------------------------------------------------------- logit adjustment --
+
+def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask, draft_tokens, logits, *,
+                  history=None, history_len=None, prompt_len=None, repetition=None, presence=None, frequency=None,
+                  bias_token=None, bias_value=None, bias_len=None, token_mask=None, mask_row=None, out=None,
+                  stream=None):
+    """Penalties for repeated tokens, biases and token masks on the logits
+    (float32 or bfloat16 [>= total_nodes, vocab]) of every tree node; see
+    d2sd_logits_args in the header. history int32 [batch, most] with
+    history_len (and prompt_len) [batch]; repetition, presence, frequency
+    float32 [batch]; bias_token int32 and bias_value float32 [batch, most] with
+    bias_len [batch]; token_mask int32 [masks, ceil(vocab / 32)] with mask_row
+    [total_nodes]. Returns out (may be logits; allocated when not given)."""
+    code = {torch.float32: F32, torch.bfloat16: BF16}.get(logits.dtype)
+    if code is None:
+        raise ValueError(f"logits dtype {logits.dtype} unsupported (float32 or bfloat16)")
+    if logits.dim() != 2 or logits.shape[0] < total_nodes:
+        raise ValueError(f"logits must be [>= {total_nodes}, vocab], got {tuple(logits.shape)}")
+    batch, vocab = node_indptr.numel() - 1, logits.shape[1]
+    if out is None:
+        out = torch.empty_like(logits)
+    if out.shape != logits.shape:
+        raise ValueError(f"out must have shape {tuple(logits.shape)}, got {tuple(out.shape)}")
+    if token_mask is not None and token_mask.shape[1] != (vocab + 31) // 32:
+        raise ValueError(f"token_mask must have {(vocab + 31) // 32} words a row, got {token_mask.shape[1]}")
+    for t, name, n in ((depth, "depth", total_nodes), (draft_tokens, "draft_tokens", total_nodes),
+                       (mask_row, "mask_row", total_nodes), (history_len, "history_len", batch),
+                       (prompt_len, "prompt_len", batch), (repetition, "repetition", batch),
+                       (presence, "presence", batch), (frequency, "frequency", batch), (bias_len, "bias_len", batch)):
+        if t is not None and t.numel() < n:
+            raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
+    for t, name in ((history, "history"), (bias_token, "bias_token"), (bias_value, "bias_value")):
+        if t is not None and (t.dim() != 2 or t.shape[0] != batch):
+            raise ValueError(f"{name} must be [{batch}, most], got {tuple(t.shape)}")
+    if bias_token is not None and (bias_value is None or bias_value.shape != bias_token.shape):
+        raise ValueError("bias_value must have bias_token's shape")
+    i32, f32 = torch.int32, torch.float32
+    a = LogitsArgs(batch, total_nodes, max_nodes, anc_mask.shape[1], vocab, code,
+                   history.shape[1] if history is not None else 0, bias_token.shape[1] if bias_token is not None else 0,
+                   token_mask.shape[0] if token_mask is not None else 0, _dev(node_indptr, "node_indptr", i32),
+                   _dev(depth, "depth", i32), _dev(anc_mask, "anc_mask", i32), _dev(draft_tokens, "draft_tokens", i32),
+                   _dev(logits, "logits"), _dev(history, "history", i32), _dev(history_len, "history_len", i32),
+                   _dev(prompt_len, "prompt_len", i32), _dev(repetition, "repetition", f32),
+                   _dev(presence, "presence", f32), _dev(frequency, "frequency", f32),
+                   _dev(bias_token, "bias_token", i32), _dev(bias_value, "bias_value", f32),
+                   _dev(bias_len, "bias_len", i32), _dev(token_mask, "token_mask", i32),
+                   _dev(mask_row, "mask_row", i32), _dev(out, "out", logits.dtype))
+    _check(_adjust(ctypes.byref(a), _stream(stream)), "d2sd_adjust_logits")
+    return out
 
 
 # ---------------------------------------------------------------- timing --
