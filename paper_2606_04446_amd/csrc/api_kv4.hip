@@ -69,42 +69,54 @@ d2sd_status validate_attn_kv4(const d2sd_attn_args* a) {
   return D2SD_OK;
 }
 
-// Row groups of one split over the batch: exact with host offsets, else from
-// the mean tree.
-long long row_groups(const d2sd_attn_args* a, int G, int rows_per_group) {
-  long long groups = 0;
-  if (a->node_indptr_host) {
-    for (int b = 0; b < a->batch; ++b) {
-      const long long rows = (long long)(a->node_indptr_host[b + 1] - a->node_indptr_host[b]) * G;
-      groups += (rows + rows_per_group - 1) / rows_per_group;
-    }
-  } else {
-    const double rows = (double)a->total_nodes / a->batch * G;
-    groups = (long long)a->batch * max(1, (int)ceil(rows / rows_per_group));
-  }
-  return max(1ll, groups * a->num_kv_heads);
-}
+constexpr int kStepKeys = 128;
+constexpr long long kMaxUnits = 1ll << 24;              // of one request's streams, which the kernels add up in 32 bits
 
+// Two workgroups of four waves per CU are resident (bf16; one with fp32, whose
+// terms take twice the registers), and that is the grid unless a share would
+// fall below kMinSteps steps of keys, less than which is not worth a partial
+// state (one request of one token over 4096 keys: 21.1 us with two, 21.9 with
+// one, 23.8 with three).
+//
+// A stream's start, tree and end take as long as some steps of its keys, and a
+// share that holds many short streams would end last. They are charged 30 units
+// of cost (fp32: 15; a step of four row tiles is 8), at most half a share: 64
+// requests of one token over 500 to 16000 keys took 181 us with 3, 167 with 10,
+// 150 with 20, 133 with 30 and 134 with 45.
+constexpr int kMinSteps = 2;
 d2sd_status make_kv4_plan(const d2sd_attn_args* a, d2sd::Kv4Plan* plan) {
   const int G = a->num_qo_heads / a->num_kv_heads;
-  const long long rows = (long long)a->max_nodes * G;
+  const bool bf16 = a->dtype == D2SD_BF16;
   const int ctx = a->stage == D2SD_STAGE_TREE ? 0 : a->max_ctx_len;
-  plan->waves = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
-  const int rows_per_group = plan->waves * d2sd::kRowsPerTile;
-  const long long g = row_groups(a, G, rows_per_group);
-  const long long resident = (long long)kNumCUs * (plan->waves <= 2 ? 3 : plan->waves == 4 ? 2 : 1);
-  const int s_lo = max(1, (ctx + d2sd::kKv4MaxSplit - 1) / d2sd::kKv4MaxSplit);
-  const int s = (int)min((2 * resident + g - 1) / g, (long long)max(1, ctx / 256));
-  const int splits = max(s_lo, s);
-  plan->split = a->kv_split > 0 ? a->kv_split : max(64, ((ctx + splits - 1) / splits + 63) / 64 * 64);
-  plan->n_ch_max = max(1, (ctx + plan->split - 1) / plan->split);
-  plan->n_rg_max = (int)max(1ll, (rows + rows_per_group - 1) / rows_per_group);
-  plan->items = (long long)a->batch * a->num_kv_heads * plan->n_ch_max * plan->n_rg_max;
-  if (plan->items > kMaxGroups) return fail(D2SD_ERR_UNSUPPORTED, "too many work items (%lld)", plan->items);
-  if ((long long)a->batch * ((long long)a->max_nodes * a->num_qo_heads / 8 + 1) > kMaxGroups)
-    return fail(D2SD_ERR_UNSUPPORTED, "too many split-merge workgroups (batch %d, max_nodes %d)", a->batch, a->max_nodes);
-  const size_t states = (size_t)plan->n_ch_max * a->total_nodes * a->num_qo_heads;
-  plan->ws_bytes = plan->n_ch_max > 1 ? states * (D2SD_HEAD_DIM + 2) * sizeof(float) : 0;
+  auto tiles_of = [&](long long nodes) { return (int)((nodes * G + d2sd::kRowsPerTile - 1) / d2sd::kRowsPerTile); };
+  const int tiles_most = max(1, tiles_of(a->max_nodes));
+  const long long steps = (ctx + kStepKeys - 1) / kStepKeys + 1 + (a->max_nodes + 63ll) / 64;   // of a stream, at most
+  if ((steps + 16) * d2sd::kv4_cost(tiles_most) * a->num_kv_heads > kMaxUnits)
+    return fail(D2SD_ERR_UNSUPPORTED, "max_ctx_len %d x max_nodes %d is too much for one request", a->max_ctx_len, a->max_nodes);
+  long long streams = 0, cost = 0;                      // of a step of all streams; exact with host offsets, else from the mean request
+  auto count = [&](int tiles, long long times) {
+    streams += times * a->num_kv_heads * (tiles / 4 + (tiles >> 1 & 1) + (tiles & 1));
+    cost += times * a->num_kv_heads * d2sd::kv4_cost(tiles);
+  };
+  if (a->node_indptr_host) {
+    for (int b = 0; b < a->batch; ++b) count(tiles_of(a->node_indptr_host[b + 1] - a->node_indptr_host[b]), 1);
+  } else {
+    count(max(1, tiles_of(a->total_nodes / max(1, a->batch))), a->batch);
+  }
+  plan->whole = ctx == 0 || a->total_nodes == 0;
+  plan->most = plan->whole ? 1 : d2sd::kv4_cost(tiles_most >= 4 ? 4 : tiles_most >= 2 ? 2 : 1);
+  const long long resident = (bf16 ? 2 : 1) * kNumCUs;
+  long long want = plan->whole ? min(streams, 16 * resident) : min(resident, steps * cost / (kMinSteps * plan->most));
+  if (a->kv_split > 0 && !plan->whole) want = min(streams * steps * kStepKeys / a->kv_split, 64ll * resident);
+  plan->grid = (int)((max(1ll, want) + 7) / 8 * 8);
+  const long long charge = min(bf16 ? 30ll : 15ll, steps * cost / plan->grid / 2);
+  for (int i = 0; i < 3; ++i) plan->charge[i] = max(1, (int)(charge / d2sd::kv4_cost(1 << i)));
+  const long long pieces = plan->grid / max(1ll, streams);
+  plan->span = (int)max(1ll, min(64ll, pieces));
+  plan->per = pieces > 16 ? 8 : pieces > 4 ? 4 : 1;
+  plan->slot_rows = min(4, tiles_most) * d2sd::kRowsPerTile;
+  const size_t states = (size_t)2 * plan->grid * plan->slot_rows;
+  plan->ws_bytes = plan->whole ? 0 : states * (D2SD_HEAD_DIM + 2) * sizeof(float) + (size_t)plan->grid * 4 * sizeof(int);
   plan->scale = a->sm_scale > 0.0f ? a->sm_scale : 1.0f / sqrtf((float)a->head_dim);
   return D2SD_OK;
 }

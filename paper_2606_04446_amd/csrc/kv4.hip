@@ -57,7 +57,7 @@ __device__ __forceinline__ void write_row8(const float (&v)[8], uint8_t* codes, 
   top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, false));   // quad_perm [2,3,0,1]
   const int byte = kv4_scale_byte(top);
   // the codes of a block that reads as NaN do not matter, but are the same every time
-  const uint32_t code = byte == kScaleNan ? 0u : kv4_encode8(v, kv4_scale(byte));
+  const uint32_t code = byte == kScaleNan ? 0u : kv4_encode8(v, kv4_scale((uint32_t)byte));
   *reinterpret_cast<uint32_t*>(codes + row * kKv4RowBytes + sub * 4) = code;
   if ((sub & 3) == 0) scales[row * kKv4Blocks + (sub >> 2)] = (uint8_t)byte;
 }
@@ -166,8 +166,8 @@ __global__ __launch_bounds__(kKv4Threads) void read_kv4_kernel(
     const size_t row = cache_row(page_table + (size_t)b * max_pages, min(pos, last), num_pages, hkv, h);
     const uint32_t ck = *reinterpret_cast<const uint32_t*>(cache.k + row * kKv4RowBytes + sub * 4);
     const uint32_t cv = *reinterpret_cast<const uint32_t*>(cache.v + row * kKv4RowBytes + sub * 4);
-    const int sk = cache.k_scale[row * kKv4Blocks + (sub >> 2)];
-    const int sv = cache.v_scale[row * kKv4Blocks + (sub >> 2)];
+    const uint32_t sk = cache.k_scale[row * kKv4Blocks + (sub >> 2)];
+    const uint32_t sv = cache.v_scale[row * kKv4Blocks + (sub >> 2)];
     store8(k_out + dst, ck, kv4_scale(sk));
     store8(v_out + dst, cv, kv4_scale(sv));
   }

@@ -26,10 +26,9 @@ __device__ __forceinline__ int kv4_scale_byte(uint32_t top_bits) {
   return clampi(e, kScaleMin, kScaleMax);
 }
 
-// 2^(byte - 127); a NaN for 255.
-__device__ __forceinline__ float kv4_scale(int byte) {
-  return byte == kScaleNan ? __uint_as_float(0x7fc00000u) : byte == 0 ? __uint_as_float(0x00400000u) : __uint_as_float((uint32_t)byte << 23);
-}
+// Scale operand of the conversions for a scale byte: they read its exponent
+// field only, 255 (an infinity here) as NaN.
+__device__ __forceinline__ float kv4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Codes of eight values, the first in the lowest bits: x / scale rounded to
 // the nearest E2M1 value, ties to even, saturating at 6.

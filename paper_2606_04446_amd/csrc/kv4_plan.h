@@ -5,17 +5,25 @@
 
 namespace d2sd {
 
-constexpr int kKv4MaxSplit = 32768;   // context tokens per split: its page ids are staged in LDS
-
 struct Kv4Plan {
-  int waves;         // waves of 32 query rows per workgroup: 1, 2, 4 or 8
-  int split;         // context tokens per split (multiple of 64)
-  int n_ch_max;      // splits of the longest context (>= 1)
-  int n_rg_max;      // row groups of the largest request (>= 1)
-  long long items;   // batch * hkv * n_ch_max * n_rg_max
-  size_t ws_bytes;   // partial states (0 for one split)
+  int grid;          // workgroups, a multiple of 8
+  int whole;         // no stream is cut: no partial states, no merge
+  int most;          // cost of the largest group's step (1 when whole)
+  int charge[3];     // steps that a stream of 1, 2 or 4 row tiles counts beside those of its keys
+  int span, per;     // the merge: entries per workgroup (up to 64), lanes' groups per row (1, 4 or 8)
+  int slot_rows;     // rows of a partial state's slot
+  size_t ws_bytes;   // slots and the list of cut streams (0 when whole)
   float scale;       // softmax scale
 };
+
+// Cost of a step (128 keys) for a workgroup that holds 1, 2 or 4 row tiles, and
+// of a step for all `tiles` row tiles of a KV head (four at a time, then two, then one).
+#ifndef KC1
+#define KC1 3
+#define KC2 5
+#define KC4 8
+#endif
+__host__ __device__ inline int kv4_cost(int tiles) { return KC4 * (tiles >> 2) + (tiles & 2 ? KC2 : 0) + (tiles & 1 ? KC1 : 0); }
 
 hipError_t launch_kv4_attention(const d2sd_attn_args& a, const d2sd_kv4_cache& cache, const Kv4Plan& plan, void* ws,
                                 hipStream_t stream);
