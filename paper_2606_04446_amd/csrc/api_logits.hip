@@ -17,8 +17,8 @@ extern "C" d2sd_status d2sd_adjust_logits(const d2sd_logits_args* a, hipStream_t
   if (a->dtype != D2SD_F32 && a->dtype != D2SD_BF16) return fail(D2SD_ERR_INVALID_ARG, "dtype %d unknown", a->dtype);
   if (a->max_history < 0 || a->max_bias < 0 || a->num_masks < 0)
     return fail(D2SD_ERR_INVALID_ARG, "max_history, max_bias and num_masks must be >= 0");
-  if ((long long)a->batch * a->max_nodes * ((a->vocab + 4095) / 4096) >= (1ll << 24))
-    return fail(D2SD_ERR_UNSUPPORTED, "batch x max_nodes x vocab / 4096 needs more than 2^24 workgroups");
+  if ((long long)a->batch * a->max_nodes * ((a->vocab + 2047) / 2048) >= (1ll << 24))
+    return fail(D2SD_ERR_UNSUPPORTED, "batch x max_nodes x vocab / 2048 needs more than 2^24 workgroups");
   if (!a->node_indptr || !a->depth || !a->anc_mask || !a->draft_tokens || !a->logits || !a->out)
     return fail(D2SD_ERR_INVALID_ARG, "a required device pointer is NULL");
   if (a->max_history > 0 && (!a->history || !a->history_len))

@@ -5,14 +5,23 @@
 // few draft tokens on their root paths, so it is y = x * (x > 0 ? mp : mn) + a
 // with mp, mn and a per (request, token). A workgroup takes a chunk of the
 // vocabulary of one request, builds these from the request's token history and
-// bias list (counted in LDS, kept in registers, 16 tokens a thread), and then
-// streams the chunk of each of its nodes' rows past them: one read and one
-// write of the logits, plus a bit per token where the node has a mask. Draft
-// tokens in the chunk are listed per owning thread; a thread with a non-empty
-// list corrects its registers for the entries that are ancestors of the node,
-// and the others never look, so the loop has no barrier. Counts are integers
-// and bias lists are summed in order, so results do not depend on timing.
-// Bound by memory: 2 bytes in and 2 out per bf16 logit.
+// bias list (counted in LDS, kept in registers, 8 tokens a thread), and then
+// streams the chunk of up to kMaxPer of its nodes' rows past them: one read and
+// one write of the logits, plus a bit per token where the node has a mask. Draft
+// tokens in the chunk are listed per owning thread, with a bit for each of the
+// workgroup's nodes that they are an ancestor of; a thread writes the tokens
+// with a node's bit once more, corrected, so the loop over the rows has no
+// barrier and seldom leaves its straight path. Counts are integers and bias
+// lists are summed in order, so results do not depend on timing.
+//
+// Bound by memory: 2 bytes in and 2 out per bf16 logit. Occupancy hides its
+// latency, so the registers of a thread decide: with 8 tokens (64 registers,
+// eight workgroups per CU) 2560 rows of 32000 bf16 logits with 4000 tokens of
+// history take 82.6 us, 4.0 TB/s, where 328 MB at a copy's rate would take 70;
+// 16 tokens (116 registers) took 96.3, and the next row's loads before this one's
+// stores (70 registers) 89.3. 128 or 512 threads: 99.2, 88.4; at most 4 or 12
+// nodes per workgroup: 98.0, 83.4. With 384 rows of 150001 logits, which start
+// at any even address, 56.9 us, 4.1 TB/s.
 #include "launchers.h"
 
 namespace d2sd {
@@ -20,9 +29,13 @@ namespace d2sd {
 namespace {
 
 constexpr int kThr = 256;
-constexpr int kElems = 16;                          // tokens per thread
+constexpr int kElems = 8;                           // tokens per thread
 constexpr int kChunk = kThr * kElems;
 constexpr int kListMax = D2SD_MAX_B + D2SD_MAX_B * (D2SD_MAX_B - 1) / 2;   // nodes of a request
+constexpr int kMaskWords = (kListMax + 31) / 32;
+constexpr int kMaxPer = 8;                          // nodes per workgroup, at most
+static_assert(kMaxPer <= 12, "bits of a list entry");
+constexpr int kBurst = 8;                           // loads of the history that a thread has in flight
 constexpr uint32_t kNoEntry = 0xfffu;
 constexpr uint32_t kPromptBit = 1u << 31;
 static_assert(kListMax < (int)kNoEntry, "list entries are linked by 12 bits");
@@ -103,9 +116,11 @@ __global__ __launch_bounds__(kThr) void adjust_logits_kernel(d2sd_logits_args a,
   constexpr int N = Vec<T>::N;                      // tokens of a 16-byte vector
   constexpr int kVecs = kElems / N;                 // vectors per thread: tokens v kThr N + t N .. + N of the chunk
   __shared__ uint32_t s_tok[kChunk];                // counts, then bias values
-  __shared__ uint32_t s_list[kListMax];             // next entry << 16 | token of the thread << 12 | node
+  __shared__ uint32_t s_list[kListMax];             // next entry << 16 | token of the thread << 12 | the nodes that it is an ancestor of
   __shared__ uint32_t s_head[kThr];
-  __shared__ int s_n;
+  __shared__ uint32_t s_anc[kMaxPer][kMaskWords];   // ancestor masks of the workgroup's nodes
+  __shared__ int s_row[kMaxPer];                    // their token masks
+  __shared__ int s_n, s_before[kThr / kWave];
 
   int rest = blockIdx.x;
   const int ck = rest % chunks; rest /= chunks;
@@ -122,6 +137,10 @@ __global__ __launch_bounds__(kThr) void adjust_logits_kernel(d2sd_logits_args a,
   // ---- what the request's history and biases make of the chunk ----
 #pragma unroll
   for (int i = 0; i < kElems; ++i) s_tok[i * kThr + t] = 0;
+  const int node_words = (nodes + 31) >> 5;
+  for (int i = t; i < (n1 - n0) * node_words; i += kThr)
+    s_anc[i / node_words][i % node_words] = a.anc_mask[(size_t)(base + n0 + i / node_words) * a.mask_words + i % node_words];
+  if (t < n1 - n0) s_row[t] = a.num_masks > 0 ? min(a.mask_row[base + n0 + t], a.num_masks - 1) : -1;
   s_head[t] = kNoEntry;
   if (t == 0) s_n = 0;
   __syncthreads();
@@ -129,23 +148,21 @@ __global__ __launch_bounds__(kThr) void adjust_logits_kernel(d2sd_logits_args a,
     const int* hist = a.history + (size_t)b * a.max_history;
     const int len = clampi(a.history_len[b], 0, a.max_history);
     const int prompt = a.prompt_len ? clampi(a.prompt_len[b], 0, len) : 0;
-    for (int i = t; i < len; i += kThr) {
-      const uint32_t off = (uint32_t)hist[i] - (uint32_t)c0;
-      if (off >= (uint32_t)here) continue;
-      if (i < prompt)
-        atomicOr(&s_tok[off], kPromptBit);
-      else
-        atomicAdd(&s_tok[off], 1u);
+    for (int i0 = t; i0 < len; i0 += kBurst * kThr) {
+      int tok[kBurst];
+#pragma unroll
+      for (int k = 0; k < kBurst; ++k) tok[k] = hist[min(i0 + k * kThr, len - 1)];
+#pragma unroll
+      for (int k = 0; k < kBurst; ++k) {
+        const int i = i0 + k * kThr;
+        const uint32_t off = (uint32_t)tok[k] - (uint32_t)c0;
+        if (i >= len || off >= (uint32_t)here) continue;
+        if (i < prompt)
+          atomicOr(&s_tok[off], kPromptBit);
+        else
+          atomicAdd(&s_tok[off], 1u);
+      }
     }
-  }
-  // draft tokens of the chunk, linked by the thread that owns them
-  for (int n = t; n < nodes; n += kThr) {
-    const uint32_t off = (uint32_t)a.draft_tokens[base + n] - (uint32_t)c0;
-    if (off >= (uint32_t)here || a.depth[base + n] <= 0) continue;
-    const int owner = (int)off % (kThr * N) / N;
-    const uint32_t e = (uint32_t)off / (kThr * N) * N + off % N;
-    const uint32_t at = (uint32_t)atomicAdd(&s_n, 1);
-    s_list[at] = atomicExch(&s_head[owner], at) << 16 | e << 12 | (uint32_t)n;
   }
   __syncthreads();
   const float rep = a.repetition ? a.repetition[b] : 1.0f;
@@ -170,75 +187,129 @@ __global__ __launch_bounds__(kThr) void adjust_logits_kernel(d2sd_logits_args a,
     const int* tok = a.bias_token + (size_t)b * a.max_bias;
     const float* val = a.bias_value + (size_t)b * a.max_bias;
     const int len = a.bias_len ? clampi(a.bias_len[b], 0, a.max_bias) : a.max_bias;
-    for (int i = t; i < len; i += kThr) {
-      const int j = tok[i];
-      const uint32_t off = (uint32_t)j - (uint32_t)c0;
-      if (off >= (uint32_t)here) continue;
-      bool first = true;                            // the token's first entry sums them all, in order
-      for (int k = 0; k < i && first; ++k) first = tok[k] != j;
-      if (!first) continue;
-      float sum = val[i];
-      for (int k = i + 1; k < len; ++k)
-        if (tok[k] == j) sum += val[k];
-      s_tok[off] = __float_as_uint(sum);
+    uint32_t* s_bias = s_list;                      // free until the list is made
+    float* s_value = reinterpret_cast<float*>(s_list + kThr);
+    static_assert(kListMax >= 2 * kThr);
+    // kThr entries at a time: those of the chunk are moved together, in order,
+    // and the first of a token adds them all, in order
+    for (int i0 = 0; i0 < len; i0 += kThr) {
+      const int i = i0 + t;
+      const uint32_t off = i < len ? (uint32_t)tok[i] - (uint32_t)c0 : ~0u;
+      const float value = i < len ? val[i] : 0.0f;
+      const bool in = off < (uint32_t)here;
+      const uint64_t vote = __ballot(in);
+      if (t % kWave == 0) s_before[t / kWave] = __popcll(vote);
+      __syncthreads();
+      int at = __popcll(vote & ((1ull << (t % kWave)) - 1ull)), all = 0;
+#pragma unroll
+      for (int w = 0; w < kThr / kWave; ++w) {
+        if (w < t / kWave) at += s_before[w];
+        all += s_before[w];
+      }
+      if (in) {
+        s_bias[at] = off;
+        s_value[at] = value;
+      }
+      __syncthreads();
+      if (t < all) {
+        const uint32_t mine = s_bias[t];
+        bool first = true;
+        for (int k = 0; k < t && first; ++k) first = s_bias[k] != mine;
+        if (first) {
+          float sum = __uint_as_float(s_tok[mine]);
+          for (int k = t; k < all; ++k)
+            if (s_bias[k] == mine) sum += s_value[k];
+          s_tok[mine] = __float_as_uint(sum);
+        }
+      }
+      __syncthreads();
     }
-    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kElems; ++i) add[i] += __uint_as_float(s_tok[i / N * (kThr * N) + t * N + i % N]);
   }
+  // draft tokens of the chunk, linked by the thread that owns them
+  for (int n = t; n < nodes; n += kThr) {
+    const uint32_t off = (uint32_t)a.draft_tokens[base + n] - (uint32_t)c0;
+    if (off >= (uint32_t)here || a.depth[base + n] <= 0) continue;
+    const int owner = (int)off % (kThr * N) / N;
+    const uint32_t e = (uint32_t)off / (kThr * N) * N + off % N;
+    const uint32_t at = (uint32_t)atomicAdd(&s_n, 1);
+    uint32_t below = 0;                             // a bit per node of the workgroup: n is its ancestor or itself
+    for (int k = 0; k < n1 - n0; ++k) below |= ((s_anc[k][n >> 5] >> (n & 31)) & 1u) << k;
+    s_list[at] = atomicExch(&s_head[owner], at) << 16 | e << 12 | below;
+  }
+  __syncthreads();
   const uint32_t head = s_head[t];
+  uint32_t below = 0;                               // the nodes that the thread has something more for
+  for (uint32_t at = head; at != kNoEntry; at = s_list[at] >> 16) below |= s_list[at] & ((1u << kMaxPer) - 1u);
 
   // ---- the rows ----
   const T* in = static_cast<const T*>(a.logits);
   T* out = static_cast<T*>(a.out);
   const int words = (a.vocab + 31) >> 5;
-  for (int n = n0; n < n1; ++n) {
-    const size_t row = (size_t)(base + n) * a.vocab;
-    const int mr = a.num_masks > 0 ? min(a.mask_row[base + n], a.num_masks - 1) : -1;
+  struct Row {
     u32x4 raw[kVecs];
     uint32_t allowed[kVecs];
+  };
+  auto fetch = [&](int n, Row& r) {
+    const size_t row = (size_t)(base + n) * a.vocab;
+    const int mr = s_row[n - n0];
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
       const int j = c0 + v * (kThr * N) + t * N;
-      allowed[v] = ~0u;
+      r.allowed[v] = ~0u;
       if (j >= a.vocab) continue;
-      raw[v] = load_vec(in + row, j, a.vocab);
-      if (mr >= 0) allowed[v] = a.token_mask[(size_t)mr * words + (j >> 5)] >> (j & 31);
+      r.raw[v] = load_vec(in + row, j, a.vocab);
+      if (mr >= 0) r.allowed[v] = a.token_mask[(size_t)mr * words + (j >> 5)] >> (j & 31);
     }
+  };
+  auto finish = [&](int n, const Row& r) {
+    const size_t row = (size_t)(base + n) * a.vocab;
+    // where x counts as a repeated token's, and what is added to it: y
+    auto adjust = [&](float x, bool repeated, float more) { return x * (repeated ? (x > 0.0f ? inv_rep : rep) : 1.0f) + more; };
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) {
       const int j = c0 + v * (kThr * N) + t * N;
       if (j >= a.vocab) continue;
       float x[N];
-      unpack(raw[v], x);
-      float y[N];
+      unpack(r.raw[v], x);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int e = v * N + i;
-        const float f = (seen >> e) & 1u ? (x[i] > 0.0f ? inv_rep : rep) : 1.0f;
-        y[i] = x[i] * f + add[e];
+        x[i] = adjust(x[i], (seen >> (v * N + i)) & 1u, add[v * N + i]);
+        if (!((r.allowed[v] >> i) & 1u)) x[i] = -INFINITY;
       }
-      for (uint32_t at = head; at != kNoEntry; at = s_list[at] >> 16) {
-        const uint32_t e = (s_list[at] >> 12) & 15u;
-        if ((int)e / N != v) continue;
-        // how many of the node's ancestors-or-self draft this token
-        int hits = 0;
-        for (uint32_t k = head; k != kNoEntry; k = s_list[k] >> 16) {
-          const uint32_t m = s_list[k] & 0xfffu;
-          if (((s_list[k] >> 12) & 15u) == e)
-            hits += (a.anc_mask[(size_t)(base + n) * a.mask_words + (m >> 5)] >> (m & 31)) & 1u;
-        }
-        if (hits == 0) continue;
-        const float more = -((float)hits * freq) - ((counted >> e) & 1u ? 0.0f : pres);
+      store_vec(out + row, j, a.vocab, pack(x));
+    }
+    if (!((below >> (n - n0)) & 1u)) return;
+    // tokens that the node or its ancestors draft, over what was written
+    for (uint32_t at = head; at != kNoEntry; at = s_list[at] >> 16) {
+      if (!((s_list[at] >> (n - n0)) & 1u)) continue;
+      const uint32_t e = (s_list[at] >> 12) & 15u;
+      int hits = 0;                                 // how many of them draft it
+      for (uint32_t k = head; k != kNoEntry; k = s_list[k] >> 16)
+        if (((s_list[k] >> 12) & 15u) == e) hits += (s_list[k] >> (n - n0)) & 1u;
+      float x = 0.0f, more = 0.0f;
+      bool allowed = true;
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) {
+        float u[N];
+        unpack(r.raw[v], u);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-          if (v * N + i == (int)e) y[i] = x[i] * (x[i] > 0.0f ? inv_rep : rep) + (add[v * N + i] + more);
+          if (e == (uint32_t)(v * N + i)) {
+            x = u[i];
+            more = add[v * N + i];
+            allowed = (r.allowed[v] >> i) & 1u;
+          }
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (!((allowed[v] >> i) & 1u)) y[i] = -INFINITY;
-      store_vec(out + row, j, a.vocab, pack(y));
+      more += -((float)hits * freq) - ((counted >> e) & 1u ? 0.0f : pres);
+      out[row + c0 + e / N * (kThr * N) + t * N + e % N] = allowed ? (T)adjust(x, true, more) : (T)-INFINITY;
     }
+  };
+  for (int n = n0; n < n1; ++n) {
+    Row r;
+    fetch(n, r);
+    finish(n, r);
   }
 }
 
@@ -249,7 +320,7 @@ hipError_t launch_adjust_logits(const d2sd_logits_args& a, hipStream_t stream) {
   // Nodes per workgroup: the history is counted once for all of them, but
   // there should be some eight workgroups for each of the 256 CUs.
   const long long rows = (long long)a.total_nodes * chunks;
-  const int per = (int)max(1ll, min(8ll, rows / 2048));
+  const int per = (int)max(1ll, min((long long)kMaxPer, rows / 2048));
   const int groups = ceil_div(a.max_nodes, per);
   const dim3 grid((unsigned)((long long)a.batch * groups * chunks));
   if (a.dtype == D2SD_BF16)
