@@ -8,16 +8,19 @@
 //    takes an E2M1 operand with a power of two per 32 elements of its
 //    contraction axis, which is how a key row is stored (blocks of 32 dims),
 //    so a lane's operand is 16 bytes of the row and one byte of its scales,
-//    with no conversion and a quarter of the LDS traffic of bf16. The queries,
-//    times the softmax scale and log2 e, are the other operand, as a sum of
-//    E2M3 terms: with u a power of two, u >= max |x| / 16 over the lane's 32
-//    dims, x / u is rounded to an integer digit in [-16, 16], and the rest
-//    times 32 gives the next digit. E2M3 holds these digits exactly (code =
-//    digit), and each term costs half a bf16 product of the same shape by time
-//    in the matrix cores. n terms leave at most 2^-5n of the block's largest
-//    (its next power of two): four for bf16 calls (2^-20; three leave 2^-15, too
-//    much for an lse in 32 bits), five for fp32 ones. The scores' accumulator
-//    starts at -m, so that they leave the product ready for exp2.
+//    with no conversion and a quarter of the LDS traffic of bf16. The queries
+//    are the other operand, as a sum of E2M3 terms: with u a power of two,
+//    u >= max |x| / 16 over the lane's 32 dims, x / u is rounded to an integer
+//    digit in [-16, 16], and the rest times 32 gives the next digit. E2M3 holds
+//    these digits exactly (code = digit), and each term costs half a bf16
+//    product of the same shape by time in the matrix cores. n terms leave at
+//    most 2^-5n of the block's largest (its next power of two). bf16 queries
+//    are 8 bits long: three terms cut nothing of elements down to 2^-7 of their
+//    block's largest, and 2^-16 of it of smaller ones; with the softmax scale
+//    multiplied in they would need four (565 us instead of 538 for 32 requests
+//    of eight row tiles over 16384 keys), so the scores are scaled instead. fp32
+//    queries take the scale and are held in five terms, 25 bits; their scores'
+//    accumulator starts at -m, so that they leave the product ready for exp2.
 //  - Values are contracted over keys, along which their scales change, so they
 //    are expanded to bf16, which holds them exactly. The expansion is a product
 //    with the identity in the block-scaled MFMA: its output has a lane's dim
@@ -48,7 +51,7 @@ template <typename T>
 struct Terms;
 template <>
 struct Terms<__bf16> {
-  static constexpr int Q = 4;   // E2M3 terms of a query
+  static constexpr int Q = 3;   // E2M3 terms of a query
   static constexpr int P = 1;   // bf16 terms of P, and of tree queries, keys and values
 };
 template <>
@@ -260,6 +263,13 @@ __device__ __forceinline__ void move_reference(float mx, float& m_run, float& l_
   for (int dt = 0; dt < 4; ++dt) o[dt] *= alpha;
   l_run *= alpha;
   m_run = m_new;
+}
+// Scores times c2 and less the reference.
+__device__ __forceinline__ f32x16 ahead(const f32x16& x, float c2, float minus_m) {
+  f32x16 s;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s[i] = fmaf(x[i], c2, minus_m);
+  return s;
 }
 // Scores less the reference to weights, in place; returns their sum.
 __device__ __forceinline__ float weigh(f32x16& s) {
@@ -723,7 +733,9 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
       const float c2 = a->p.c2;
       Copies copies(a, b, h, c0, c1);
       Query<NQ> q;
-      load_query<T, NQ>(q, q_ptr, hf, c2);
+      // bf16 queries stay as they are, so that three terms hold them, and their scores are scaled
+      constexpr bool kScaled = sizeof(T) == 4;
+      load_query<T, NQ>(q, q_ptr, hf, kScaled ? c2 : 1.0f);
       sync_keep<0>();
       const int k_at0 = code_at(lane & 31, hf), k_at1 = code_at(lane & 31, 2 + hf);
       // halves of the identity: 1.0 (code 2) at dim lane % 32 of the first or of the second 32 dims
@@ -735,7 +747,7 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
         unit[0] = hf ? zero4() : e;
         unit[1] = hf ? e : zero4();
       }
-      f32x16 less = {};                                // -m in all slots: the scores' initial value
+      f32x16 less = {};                                // -m in all slots: the initial value of scaled scores
       if (m_run != -INFINITY) less -= m_run;
       // One tile; `steady`: the next one is whole and there is one to copy.
       auto step = [&](int j, auto steady) {
@@ -773,14 +785,15 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
               }
               return x;
             };
-            f32x16 s = scores(less);
+            f32x16 x = scores(kScaled ? less : f32x16{}), s = x;
+            if constexpr (!kScaled) s = ahead(x, c2, less[0]);
             float l = weigh(s);
             if (__ballot(!(l <= kMostWeight)) || (!steady.value && j == 0 && kb == ph)) {
-              f32x16 x[1] = {scores(f32x16{})};
-              move_reference(max_score<1>(x), m_run, l_run, o);
+              f32x16 y[1] = {kScaled ? scores(f32x16{}) : x * c2};
+              move_reference(max_score<1>(y), m_run, l_run, o);
               const float m0 = m_run == -INFINITY ? 0.0f : m_run;
               less = f32x16{} - m0;
-              s = x[0] - m0;
+              s = kScaled ? y[0] - m0 : ahead(x, c2, -m0);
               l = weigh(s);
             }
             l_run += l;
