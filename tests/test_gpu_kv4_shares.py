@@ -1,0 +1,81 @@
+"""How the work of an attention over a 4-bit cache is cut: batches of more
+requests than a wave has lanes, every number of row tiles, streams of many
+pieces, a workspace that an earlier call has used, calls on two streams."""
+
+import numpy as np
+import pytest
+import torch
+
+from tests.gpu_cases import d2sd
+from tests.test_gpu_kv4_attention import Batch, Rows, canonical, tokens
+
+pytestmark = pytest.mark.gpu
+
+
+def chain(n):
+    return Rows(np.tril(np.ones((n, n), bool)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv_split", [0, 128])
+def test_more_requests_than_lanes(kv_split, dtype):
+    """150 requests, of which some have no nodes or no context, with the first and the last ones empty."""
+    rng = np.random.default_rng(40)
+    nodes = rng.integers(0, 30, 150)
+    nodes[[0, 63, 64, 127, 128, 149]] = 0
+    ctx = rng.integers(0, 400, 150)
+    ctx[rng.random(150) < 0.2] = 0
+    b = Batch([chain(int(n)) for n in nodes], ctx, 4, 1, dtype, seed=41)
+    b.check(*b.run(kv_split=kv_split))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv_split", [0, 64, 256])
+def test_every_number_of_row_tiles(kv_split, dtype):
+    """One to nine tiles of 32 rows: groups of four, two and one, full and ragged."""
+    trees = [chain(8 * t - 3 * (t % 2)) for t in range(1, 10)]
+    ctx = [300, 129, 0, 513, 64, 128, 700, 1, 257]
+    b = Batch(trees, ctx, 8, 2, dtype, seed=42)
+    b.check(*b.run(kv_split=kv_split))
+    b.check(*b.run(kv_split=kv_split, node_indptr_host=b.ip))
+
+
+@pytest.mark.parametrize("kv_split", [0, 64, 704])
+def test_streams_of_many_pieces(kv_split):
+    """One stream over all workgroups: up to 264 pieces."""
+    b = Batch([chain(5)], [33700], 4, 1, "bf16", seed=43)
+    b.check(*b.run(kv_split=kv_split))
+
+
+def test_a_used_workspace_and_its_need():
+    """Larger and smaller calls in turn on one workspace, which holds junk at first; with a byte too few it is refused."""
+    m = d2sd()
+    calls = [Batch(canonical(16, [[3, 9], [1], [2, 4, 8]]), [1000, 517, 64], 8, 2, "bf16", seed=44),
+             Batch(tokens(3), [2000, 40, 333], 8, 2, "bf16", seed=45),
+             Batch([chain(70)], [129], 8, 2, "bf16", seed=46)]
+    ws = torch.randint(0, 256, (1 << 24,), dtype=torch.uint8, device="cuda")
+    want = [[t.clone() for t in b.run()] for b in calls]
+    for i in (0, 1, 2, 1, 0, 2):
+        out, lse = calls[i].run(workspace=ws)
+        assert torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1])
+    b = calls[0]
+    a = m.attn_args_kv4(b.q, b.cache, b.d[0], b.d[1], b.kt, b.vt, b.d[2], b.mask, torch.empty_like(b.q), None,
+                        total_nodes=b.total, max_nodes=b.most, max_ctx_len=1000)
+    need = m.cascade_workspace_size_kv4(a)
+    out, _ = b.run(workspace=ws[:need])
+    assert torch.equal(out, want[0][0])
+    with pytest.raises(m.D2SDError):
+        b.run(workspace=ws[:need - 1])
+
+
+def test_calls_on_two_streams():
+    """Two calls at once, each with its own workspace."""
+    calls = [Batch(canonical(16, [[3, 9], [1], [2, 4, 8]]), [3000, 1517, 64], 8, 2, t, seed=47) for t in ("bf16", "f32")]
+    want = [[t.clone() for t in b.run()] for b in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got = [b.run(stream=s) for b, s in zip(calls, streams)]
+        torch.cuda.synchronize()
+        for (o, l), (x, y) in zip(got, want):
+            assert torch.equal(o, x) and torch.equal(l, y)
