@@ -176,6 +176,17 @@ def _stream(stream):
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _empty(stream, shape, dtype, device):
+    """A tensor for the stream that a call runs on: memory of that stream's own,
+    so that neither earlier nor later work of another one uses it at once."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _dev(t, name, dtype=None):
     """Device pointer of a contiguous CUDA tensor (None passes NULL)."""
     if t is None:
@@ -548,8 +559,8 @@ def read_kv4(token_indptr, total_tokens: int, max_tokens: int, page_table, cache
     """The values a 4-bit cache stands for: row token_indptr[b] + t is position
     start[b] + t of request b. Returns (k, v) [total_tokens, kv heads, 128]."""
     shape = (total_tokens, cache.num_kv_heads, HEAD_DIM)
-    k = k_out if k_out is not None else torch.empty(shape, dtype=dtype, device=cache.k.device)
-    v = v_out if v_out is not None else torch.empty(shape, dtype=k.dtype, device=cache.k.device)
+    k = k_out if k_out is not None else _empty(stream, shape, dtype, cache.k.device)
+    v = v_out if v_out is not None else _empty(stream, shape, k.dtype, cache.k.device)
     code = _rows_code(k, "k_out", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v_out", total_tokens, cache.num_kv_heads, k.dtype)
     i32 = torch.int32
@@ -597,16 +608,16 @@ def cascade_verify_attention_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree
     """Verify attention with the context in a 4-bit cache; returns (out, lse).
     The workspace is allocated when not given."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(stream, q.shape, q.dtype, q.device)
     if lse is None and want_lse:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        lse = _empty(stream, q.shape[:2], torch.float32, q.device)
     a = attn_args_kv4(q, cache, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, out, lse,
                       total_nodes=total_nodes, max_nodes=max_nodes, max_ctx_len=max_ctx_len, stage=stage,
                       sm_scale=sm_scale, kv_split=kv_split, node_indptr_host=node_indptr_host)
     if workspace is None:      # a given one is checked against the call's need by the library
         need = cascade_workspace_size_kv4(a)
         if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = _empty(stream, need, torch.uint8, q.device)
     ws_ptr = _dev(workspace, "workspace") if workspace is not None else None
     ws_len = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_cascade_kv4(ctypes.byref(a), cache.pointers, ws_ptr, ws_len, _stream(stream)),
@@ -634,7 +645,7 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
         raise ValueError(f"logits must be [>= {total_nodes}, vocab], got {tuple(logits.shape)}")
     batch, vocab = node_indptr.numel() - 1, logits.shape[1]
     if out is None:
-        out = torch.empty_like(logits)
+        out = _empty(stream, logits.shape, logits.dtype, logits.device)
     if out.shape != logits.shape:
         raise ValueError(f"out must have shape {tuple(logits.shape)}, got {tuple(out.shape)}")
     if token_mask is not None and token_mask.shape[1] != (vocab + 31) // 32:
