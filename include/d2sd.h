@@ -645,8 +645,9 @@ d2sd_status d2sd_adjust_logits(const d2sd_logits_args* args, hipStream_t stream)
 /* ------------------------------------------------------------ profiling -- */
 
 /*
- * Host. When enabled (nonzero), d2sd_cascade_verify_attention and
- * d2sd_noncascade_verify_attention record HIP events on their stream before
+ * Host. When enabled (nonzero), d2sd_cascade_verify_attention,
+ * d2sd_cascade_verify_attention_kv4 and d2sd_noncascade_verify_attention
+ * record HIP events on their stream before
  * their main (context-streaming) kernel, after it, and after the split merge
  * that follows it when the context is split. d2sd_kernel_timing_collect
  * waits for the recorded events, returns the call count and the summed

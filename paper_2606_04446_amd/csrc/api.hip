@@ -69,6 +69,10 @@ hipEvent_t take_event() {
   return e;
 }
 
+}  // namespace
+
+namespace d2sd {
+
 // Reserve three events when timing is on (all null otherwise).
 void timing_begin(hipEvent_t (&ev)[3]) {
   ev[0] = ev[1] = ev[2] = nullptr;
@@ -93,6 +97,13 @@ void timing_end(hipEvent_t (&ev)[3], bool launched, bool merged) {
   else
     for (auto& e : ev) g_event_pool.push_back(e);
 }
+
+}  // namespace d2sd
+
+namespace {
+
+using d2sd::timing_begin;
+using d2sd::timing_end;
 
 // Wait for every recorded call and return, in call order, the main kernel's
 // duration and the split merge's (ms; 0 when the call had no merge);

@@ -208,7 +208,11 @@ d2sd_status d2sd_cascade_verify_attention_kv4(const d2sd_attn_args* args, const 
   if (args->total_nodes == 0) return ok();
   if (plan.ws_bytes > 0 && reinterpret_cast<uintptr_t>(ws) % 16 != 0)
     return fail(D2SD_ERR_INVALID_ARG, "ws is not 16-byte aligned");
-  return hip_status(d2sd::launch_kv4_attention(*args, *cache, plan, ws, stream), "kv4 attention launch");
+  hipEvent_t ev[3];
+  d2sd::timing_begin(ev);
+  const hipError_t e = d2sd::launch_kv4_attention(*args, *cache, plan, ws, stream, ev);
+  d2sd::timing_end(ev, e == hipSuccess, !plan.whole);
+  return hip_status(e, "kv4 attention launch");
 }
 
 }  // extern "C"

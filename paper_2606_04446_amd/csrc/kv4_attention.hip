@@ -963,7 +963,7 @@ __global__ __launch_bounds__(kThreads) void kv4_merge_kernel(Kv4Params kp) {
 }  // namespace
 
 hipError_t launch_kv4_attention(const d2sd_attn_args& a, const d2sd_kv4_cache& cache, const Kv4Plan& plan, void* ws,
-                                hipStream_t stream) {
+                                hipStream_t stream, hipEvent_t (&ev)[3]) {
   Params p{};
   p.q = a.q; p.page_table = a.page_table; p.ctx_len = a.ctx_len; p.k_tree = a.k_tree; p.v_tree = a.v_tree;
   p.node_indptr = a.node_indptr; p.anc_mask = a.anc_mask; p.out = a.out; p.lse = a.lse;
@@ -981,11 +981,15 @@ hipError_t launch_kv4_attention(const d2sd_attn_args& a, const d2sd_kv4_cache& c
   const dim3 grid((unsigned)plan.grid), mgrid((unsigned)((plan.grid + plan.span - 1) / plan.span * (plan.slot_rows * plan.per / kMergeRows)));
   hipError_t e = hipSuccess;
   auto launch = [&](auto kernel, auto merge) {
+    if (ev[0]) (void)hipEventRecord(ev[0], stream);
     hipLaunchKernelGGL(kernel, grid, dim3(4 * kWave), 0, stream, kp);
     e = hipGetLastError();
-    if (e != hipSuccess || plan.whole) return;
+    if (e != hipSuccess) return;
+    if (ev[1]) (void)hipEventRecord(ev[1], stream);
+    if (plan.whole) return;
     hipLaunchKernelGGL(merge, mgrid, dim3(kThreads), 0, stream, kp);
     e = hipGetLastError();
+    if (ev[2]) (void)hipEventRecord(ev[2], stream);
   };
   if (a.dtype == D2SD_BF16) launch(kv4_attention_kernel<__bf16>, kv4_merge_kernel<__bf16>);
   else launch(kv4_attention_kernel<float>, kv4_merge_kernel<float>);

@@ -24,6 +24,6 @@ struct Kv4Plan {
 __host__ __device__ inline int kv4_cost(int tiles) { return 8 * (tiles >> 2) + (tiles & 2 ? 5 : 0) + (tiles & 1 ? 3 : 0); }
 
 hipError_t launch_kv4_attention(const d2sd_attn_args& a, const d2sd_kv4_cache& cache, const Kv4Plan& plan, void* ws,
-                                hipStream_t stream);
+                                hipStream_t stream, hipEvent_t (&ev)[3]);
 
 }  // namespace d2sd

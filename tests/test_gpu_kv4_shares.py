@@ -79,3 +79,19 @@ def test_calls_on_two_streams():
         torch.cuda.synchronize()
         for (o, l), (x, y) in zip(got, want):
             assert torch.equal(o, x) and torch.equal(l, y)
+
+
+def test_kernel_timing_counts_the_calls():
+    m = d2sd()
+    b = Batch(canonical(16, [[3, 9], [1]]), [3000, 517], 8, 2, "bf16", seed=48)
+    m.kernel_timing_enable(True)
+    try:
+        m.kernel_timing_collect()
+        b.run()
+        b.run(stage=m.STAGE_TREE)
+        b.run()
+        kernel, merge = m.kernel_timing_collect_parts()
+    finally:
+        m.kernel_timing_enable(False)
+    assert len(kernel) == 3 and min(kernel) > 0
+    assert merge[0] > 0 and merge[1] == 0 and merge[2] > 0
