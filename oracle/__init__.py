@@ -20,6 +20,10 @@ Each function computes the plain definition of its step, slowly and visibly:
   sampling   verification at T > 0 (Tables 3-4 report T = 1; the tree rule is
              a reading): one target draw per distinct context by inversion,
              then the greedy longest-path rule on the drawn tokens
+  kv4        the 4-bit cache: blocks of 32 values as E2M1 levels times a power
+             of two, packed codes and scale bytes, and the values they stand for
+  logits     penalties for repeated tokens, biases and token masks on a node's
+             logits, from the request's history and the node's root path
 
 Readings of points the paper leaves open are listed with each function.
 """

@@ -116,7 +116,7 @@ d2sd_status make_kv4_plan(const d2sd_attn_args* a, d2sd::Kv4Plan* plan) {
   plan->per = pieces > 16 ? 8 : pieces > 4 ? 4 : 1;
   plan->slot_rows = min(4, tiles_most) * d2sd::kRowsPerTile;
   const size_t states = (size_t)2 * plan->grid * plan->slot_rows;
-  plan->ws_bytes = plan->whole ? 0 : states * (D2SD_HEAD_DIM + 2) * sizeof(float) + (size_t)plan->grid * 4 * sizeof(int);
+  plan->ws_bytes = plan->whole ? 0 : states * (D2SD_HEAD_DIM + 2) * sizeof(float) + (size_t)plan->grid * d2sd::kKv4CutBytes;
   plan->scale = a->sm_scale > 0.0f ? a->sm_scale : 1.0f / sqrtf((float)a->head_dim);
   return D2SD_OK;
 }

@@ -29,6 +29,18 @@
 //  - The tree's own keys and values arrive in the call's type: they are taken
 //    as one (bf16) or three (fp32) bf16 planes through the bf16 MFMA.
 // Sums, maxima and outputs are fp32 throughout, partial states as well.
+//
+// What bounds it. Few rows: the cache's bytes; 64 requests of one token over 500
+// to 16000 keys (576 MB) take 130 us, 4.4 TB/s, where a plain sum over memory
+// reaches 4.0 and a copy 4.7. Many rows: 32 requests of eight row tiles over
+// 16384 keys take 538 us, 1024 TFLOP/s of the products asked for; 18 matrix
+// instructions per 32 keys and row tile, 15 ns each at the clock that they leave,
+// are 270 of it, and the 16 exponentials and 74 other vector operations beside
+// them overlap only in part (one wave per SIMD takes 670 us, two 566 with four
+// query terms). Tried and slower: V expanded once per workgroup and read back
+// transposed from LDS (545 against 571 of that version, but 246 against 233 with
+// one row tile), the next scores' products ahead of a tile's exponentials (549,
+// spilled), 64-key steps (same), three or four shares per CU (589, 598).
 #include <math.h>
 
 #include <type_traits>
@@ -310,6 +322,13 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // cost, so every workgroup has the same share whatever the lengths are, and at
 // most two of its pieces are parts of a stream. These leave their state in a
 // slot, and the merge joins the slots of every stream that was cut.
+struct CutStream {
+  int4 rows;           // first node of its request, KV head, first row of the group, rows
+  int pieces;          // 0: none
+  int unused[3];
+};
+static_assert(sizeof(CutStream) == kKv4CutBytes);
+
 struct Kv4Params {
   Params p;
   d2sd_kv4_cache cache;
@@ -318,7 +337,7 @@ struct Kv4Params {
   int most;            // cost of the largest group's step
   int charge[3];       // steps that a stream of 1, 2 or 4 tiles counts beside those of its keys
   int span, per;       // of the merge
-  int* desc;           // [G][4]: the cut stream whose second piece a workgroup holds: request, stream, pieces, -
+  CutStream* cut;      // [G]: the stream whose second piece a workgroup holds
 };
 
 constexpr int kKeys = 128;   // context keys per step
@@ -513,7 +532,7 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
     units = units_of(b0);
     W += lane_of(wave_scan<false>(units), kWave - 1);
   }
-  if (kp.desc && tid == 0) kp.desc[4 * wg + 2] = 0;
+  if (kp.cut && tid == 0) kp.cut[wg].pieces = 0;
   // no share is smaller than a step: none is empty, and a stream's pieces are consecutive workgroups
   const int grid = (int)min((long long)kp.grid, max(W / kp.most, min(W, 1ll)));
   if (wg >= grid) return;
@@ -564,11 +583,11 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
     const bool cut = u1 - u0 < steps;
     pos = min(end, beyond);
     if (u0 >= u1) continue;                           // the rest of a step that another workgroup does
-    if (u0 > 0 && tid == 0 && kp.desc) {              // a second piece: the merge starts from here
+    if (u0 > 0 && tid == 0 && kp.cut) {              // a second piece: the merge starts from here
       if (begin >= shares.start(wg - 1)) {
-        kp.desc[4 * wg] = b;
-        kp.desc[4 * wg + 1] = h * groups_of(rq.tiles) + rg;
-        kp.desc[4 * wg + 2] = shares.holder(beyond - cost, wg) - wg + 2;
+        const int r0 = group.first * kRowsPerTile;
+        kp.cut[wg].rows = make_int4(rq.base, h, r0, min(rq.nodes * p.G - r0, R * kRowsPerTile));
+        kp.cut[wg].pieces = shares.holder(beyond - cost, wg) - wg + 2;
       }
     }
 
@@ -910,14 +929,15 @@ __global__ __launch_bounds__(kThreads) void kv4_merge_kernel(Kv4Params kp) {
   const int i0 = (int)(blockIdx.x / chunks) * kp.span, lane = threadIdx.x & (kWave - 1);
   const int grp = threadIdx.x / 32, d0 = (threadIdx.x & 31) * 4;
   const int rr = (int)(blockIdx.x % chunks) * rows_here + grp / per;
-  const int pieces = lane < kp.span && i0 + lane < kp.grid ? kp.desc[4 * (i0 + lane) + 2] : 0;
+  int pieces = 0;
+  int4 of = make_int4(0, 0, 0, 0);
+  if (lane < kp.span && i0 + lane < kp.grid) {
+    pieces = kp.cut[i0 + lane].pieces;
+    of = kp.cut[i0 + lane].rows;
+  }
   for (uint64_t found = __ballot(pieces >= 2); found; found &= found - 1) {
     const int at = __ffsll((long long)found) - 1, i = i0 + at, n = lane_of(pieces, at);
-    const int b = kp.desc[4 * i], stream = kp.desc[4 * i + 1];
-    const RequestPlan rq = plan_of(kp, lengths_of(kp, b));
-    const int groups = groups_of(rq.tiles), h = stream / groups;
-    const Group group = group_of(rq.tiles, stream % groups);
-    const int r_lo = group.first * kRowsPerTile, rows = min(rq.nodes * p.G - r_lo, group.R * kRowsPerTile);
+    const int base = lane_of(of.x, at), h = lane_of(of.y, at), r_lo = lane_of(of.z, at), rows = lane_of(of.w, at);
     const bool there = rr < rows;
     float M = -INFINITY, L = 0.0f, acc[4] = {0.f, 0.f, 0.f, 0.f};
     auto fold = [&](float m, float l, const float4& v) {
@@ -951,7 +971,7 @@ __global__ __launch_bounds__(kThreads) void kv4_merge_kernel(Kv4Params kp) {
     }
     if (!there || grp % per) continue;
     const int r = r_lo + rr;
-    const size_t row = (size_t)(rq.base + r / p.G) * p.hq + h * p.G + r % p.G;
+    const size_t row = (size_t)(base + r / p.G) * p.hq + h * p.G + r % p.G;
     const float inv = L == 0.0f ? 0.0f : 1.0f / L;
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] *= inv;
@@ -977,7 +997,7 @@ hipError_t launch_kv4_attention(const d2sd_attn_args& a, const d2sd_kv4_cache& c
   p.stage = a.stage; p.total_nodes = a.total_nodes; p.max_nodes = a.max_nodes; p.max_ctx = a.max_ctx_len;
   p.num_pages = a.num_pages; p.max_pages = a.max_pages; p.mask_words = a.mask_words;
   p.c2 = plan.scale * kLog2e;
-  const Kv4Params kp{p, cache, plan.grid, plan.whole, plan.most, {plan.charge[0], plan.charge[1], plan.charge[2]}, plan.span, plan.per, ws && !plan.whole ? reinterpret_cast<int*>(p.ws_l + states) : nullptr};
+  const Kv4Params kp{p, cache, plan.grid, plan.whole, plan.most, {plan.charge[0], plan.charge[1], plan.charge[2]}, plan.span, plan.per, ws && !plan.whole ? reinterpret_cast<CutStream*>(p.ws_l + states) : nullptr};
   const dim3 grid((unsigned)plan.grid), mgrid((unsigned)((plan.grid + plan.span - 1) / plan.span * (plan.slot_rows * plan.per / kMergeRows)));
   hipError_t e = hipSuccess;
   auto launch = [&](auto kernel, auto merge) {

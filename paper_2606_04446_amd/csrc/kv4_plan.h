@@ -5,6 +5,8 @@
 
 namespace d2sd {
 
+constexpr size_t kKv4CutBytes = 32;   // of an entry of the list of cut streams
+
 struct Kv4Plan {
   int grid;          // workgroups, a multiple of 8
   int whole;         // no stream is cut: no partial states, no merge
