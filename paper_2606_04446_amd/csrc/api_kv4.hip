@@ -78,12 +78,30 @@ constexpr long long kMaxUnits = 1ll << 24;              // of one request's stre
 // state (one request of one token over 4096 keys: 21.1 us with two, 21.9 with
 // one, 23.8 with three).
 //
-// A stream's start, tree and end take as long as some steps of its keys, and a
-// share that holds many short streams would end last. They are charged 30 units
-// of cost (fp32: 15; a step of four row tiles is 8), at most half a share: 64
-// requests of one token over 500 to 16000 keys took 181 us with 3, 167 with 10,
-// 150 with 20, 133 with 30 and 134 with 45.
+// A stream's start, tree and end take as long as some steps of its keys, 10 to
+// 15 us, and a share that holds many short streams would end last. They are
+// charged kCharge units of cost (a step of four row tiles is 8), at most a
+// share: 64 requests of one token over 500 to 16000 keys took 181 us with 3,
+// 167 with 10, 150 with 20, 129 with 30 and 132 with 45.
 constexpr int kMinSteps = 2;
+constexpr long long kCharge = 30;
+
+// Whether streams that are not cut, one workgroup each, end sooner. In units of
+// cost, uncut they take, per round of resident workgroups, a start and the
+// longest stream's steps; cut, a start and one more per stream of a share, the
+// share (contexts of three quarters of the largest) and the merge, whose states
+// grow with the rows. fp32 steps count for a quarter more. us cut, uncut: 64
+// requests of one token over 100 to 2000 keys 45, 32 (over 500 to 16000 the
+// longest stream alone takes 165, all shares 129); 24 over 100 to 1000 27, 20; 16
+// of six row tiles over 500 keys 42, 27, 32 over 1000 70, 51, 64 over 100 to 500
+// 92, 74; fp32, 6 of one token and two KV heads over 706 keys 20, 28.
+bool whole_pays(bool bf16, long long streams, long long resident, long long steps, long long cost, int most, int grid) {
+  const double step = bf16 ? 1.0 : 1.25;
+  const double uncut = fmax(1.0, (double)streams / resident) * (kCharge + step * steps * most);
+  const double cut = kCharge * (1.0 + (double)streams / grid) + 0.75 * step * steps * cost / grid + 5.0 * most;
+  return uncut <= cut;
+}
+
 d2sd_status make_kv4_plan(const d2sd_attn_args* a, d2sd::Kv4Plan* plan) {
   const int G = a->num_qo_heads / a->num_kv_heads;
   const bool bf16 = a->dtype == D2SD_BF16;
@@ -103,13 +121,15 @@ d2sd_status make_kv4_plan(const d2sd_attn_args* a, d2sd::Kv4Plan* plan) {
   } else {
     count(max(1, tiles_of(a->total_nodes / max(1, a->batch))), a->batch);
   }
-  plan->whole = ctx == 0 || a->total_nodes == 0;
-  plan->most = plan->whole ? 1 : d2sd::kv4_cost(tiles_most >= 4 ? 4 : tiles_most >= 2 ? 2 : 1);
+  const int most = d2sd::kv4_cost(tiles_most >= 4 ? 4 : tiles_most >= 2 ? 2 : 1);
   const long long resident = (bf16 ? 2 : 1) * kNumCUs;
-  long long want = plan->whole ? min(streams, 16 * resident) : min(resident, steps * cost / (kMinSteps * plan->most));
-  if (a->kv_split > 0 && !plan->whole) want = min(streams * steps * kStepKeys / a->kv_split, 64ll * resident);
-  plan->grid = (int)((max(1ll, want) + 7) / 8 * 8);
-  const long long charge = min(bf16 ? 30ll : 15ll, steps * cost / plan->grid / 2);
+  auto rounded = [](long long want) { return (int)((max(1ll, want) + 7) / 8 * 8); };
+  const int cut_grid = rounded(a->kv_split > 0 ? min(streams * steps * kStepKeys / a->kv_split, 64 * resident)
+                                               : min(resident, steps * cost / (kMinSteps * most)));
+  plan->whole = ctx == 0 || a->total_nodes == 0 || (a->kv_split == 0 && whole_pays(bf16, streams, resident, steps, cost, most, cut_grid));
+  plan->most = plan->whole ? 1 : most;
+  plan->grid = plan->whole ? rounded(min(streams, 16 * resident)) : cut_grid;
+  const long long charge = min(kCharge, steps * cost / plan->grid);
   for (int i = 0; i < 3; ++i) plan->charge[i] = max(1, (int)(charge / d2sd::kv4_cost(1 << i)));
   const long long pieces = plan->grid / max(1ll, streams);
   plan->span = (int)max(1ll, min(64ll, pieces));

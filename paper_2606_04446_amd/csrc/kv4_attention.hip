@@ -600,7 +600,7 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
     const bool valid = r < r_hi;
     const int node = valid ? r / p.G : 0;
     const int qrow = valid ? (node_base + node) * p.hq + h * p.G + r % p.G : -1;
-    const int t0 = max(0, u0 - pre), t1 = kp.whole ? 0 : max(0, u1 - pre);   // context tiles
+    const int t0 = kp.whole ? 0 : max(0, u0 - pre), t1 = kp.whole ? ceil_div(rq.ctx, kKeys) : max(0, u1 - pre);   // context tiles
     const int c0 = t0 * kKeys, c1 = min(rq.ctx, t1 * kKeys);
 
     // the first tiles start on their way

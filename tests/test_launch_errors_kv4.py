@@ -18,7 +18,7 @@ P = ctypes.c_void_p(1 << 20)
 cache = d2sd.Kv4Pointers(*(1 << 20,) * 4)
 attn = lambda **kw: d2sd.AttnArgs(**{**dict(
     batch=2, num_qo_heads=8, num_kv_heads=2, head_dim=128, page_size=16, dtype=d2sd.BF16, stage=d2sd.STAGE_CASCADE,
-    total_nodes=40, max_nodes=20, max_ctx_len=500, num_pages=64, max_pages=32, mask_words=1, q=1 << 20, page_table=1 << 20,
+    total_nodes=40, max_nodes=20, max_ctx_len=30000, num_pages=2048, max_pages=2000, mask_words=1, q=1 << 20, page_table=1 << 20,
     ctx_len=1 << 20, k_tree=1 << 20, v_tree=1 << 20, node_indptr=1 << 20, anc_mask=1 << 20, out=1 << 20, lse=None), **kw})
 def attend(**kw):
     a = attn(**kw)
@@ -30,6 +30,8 @@ calls = {
     "commit": (1, lambda: d2sd._commit_kv4(2, 8, 2, 128, 16, d2sd.BF16, 64, 32, 100, P, 40, P, P, P, P, P, P, ctypes.byref(cache), None)),
     "read": (1, lambda: d2sd._read_kv4(2, 2, 128, 16, d2sd.BF16, 64, 32, P, 30, 20, None, P, ctypes.byref(cache), P, P, None)),
     "attention": (2, attend), "attention, fp32": (2, lambda: attend(dtype=d2sd.F32)),
+    "attention, short contexts": (1, lambda: attend(max_ctx_len=100)),
+    "attention, short contexts cut": (2, lambda: attend(max_ctx_len=500, kv_split=64)),
     "attention, tree alone": (1, lambda: attend(stage=d2sd.STAGE_TREE)),
 }
 for name, (launches, call) in calls.items():
