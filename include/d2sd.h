@@ -578,10 +578,16 @@ d2sd_status d2sd_cascade_workspace_size_kv4(const d2sd_attn_args* args, size_t* 
  * same queries, tree keys and values, masks, stages and outputs; the context
  * keys and values are those that `cache` stands for. One token a request (a
  * tree of one node) is plain decoding. args->k_cache and args->v_cache must be
- * NULL, args->row_group and args->packed 0. kv_split as there. Products are
- * taken with the scales applied exactly and accumulated in fp32.
+ * NULL, args->row_group and args->packed 0. kv_split 0 lets the library choose
+ * between one workgroup per row group and equal shares of all keys; a multiple
+ * of 64 asks for shares of about that many keys. Products are taken with the
+ * scales applied exactly and accumulated in fp32. Results do not depend on
+ * what else runs, nor on the workspace's contents, and nothing is kept in it.
  * A tree value that is infinite or NaN reaches the rows that see its node and
- * no other. A row that sees no key gets out = 0, lse = -inf.
+ * no other. A row that sees no key gets out = 0, lse = -inf. Errors: as there;
+ * UNSUPPORTED also above about 2^28 of (max_ctx_len / 128 + max_nodes / 64 +
+ * 18) * max_nodes * num_qo_heads (250000 tokens of context with 2080 nodes and
+ * 64 query heads).
  */
 d2sd_status d2sd_cascade_verify_attention_kv4(const d2sd_attn_args* args, const d2sd_kv4_cache* cache, void* ws,
                                               size_t ws_bytes, hipStream_t stream);
@@ -638,7 +644,8 @@ typedef struct d2sd_logits_args {
  * Device. Adjusts the logits of every tree node (see d2sd_logits_args) for
  * d2sd_sample_targets or an argmax. A row whose mask leaves nothing is all
  * -inf, for which d2sd_sample_targets gives -1. One launch, no workspace.
- * Errors: INVALID_ARG before any launch.
+ * Errors: INVALID_ARG, or UNSUPPORTED from 2^24 of batch * max_nodes *
+ * ceil(vocab / 2048) on, before any launch.
  */
 d2sd_status d2sd_adjust_logits(const d2sd_logits_args* args, hipStream_t stream);
 

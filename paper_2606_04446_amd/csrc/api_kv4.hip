@@ -124,7 +124,7 @@ d2sd_status make_kv4_plan(const d2sd_attn_args* a, d2sd::Kv4Plan* plan) {
   const int most = d2sd::kv4_cost(tiles_most >= 4 ? 4 : tiles_most >= 2 ? 2 : 1);
   const long long resident = (bf16 ? 2 : 1) * kNumCUs;
   auto rounded = [](long long want) { return (int)((max(1ll, want) + 7) / 8 * 8); };
-  const int cut_grid = rounded(a->kv_split > 0 ? min(streams * steps * kStepKeys / a->kv_split, 64 * resident)
+  const int cut_grid = rounded(a->kv_split > 0 ? min(streams * steps * kStepKeys / a->kv_split, 16 * resident)
                                                : min(resident, steps * cost / (kMinSteps * most)));
   plan->whole = ctx == 0 || a->total_nodes == 0 || (a->kv_split == 0 && whole_pays(bf16, streams, resident, steps, cost, most, cut_grid));
   plan->most = plan->whole ? 1 : most;

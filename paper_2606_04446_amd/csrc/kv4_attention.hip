@@ -315,8 +315,9 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // and what is left as two and one: the four waves of a workgroup hold a row tile
 // each, or share the keys of two or of one, so that none is idle. A stream is
 // such a group of R tiles with all keys that they see. It has one step per tile
-// of kKeys context keys and, before them, 1 + ceil(nodes / 64) for its start,
-// its end and the tree. A step of R tiles is taken to cost cost_of(R). All
+// of kKeys context keys and, before them, charge_of(R) steps for its start, its
+// end and the tree, and one per 64 nodes beyond the first. A step of R tiles
+// costs kv4_cost(R). All
 // streams form one line, request by request and head by head, and workgroup i
 // of G takes the steps that begin in [i W / G, (i + 1) W / G) of its W units of
 // cost, so every workgroup has the same share whatever the lengths are, and at
@@ -519,6 +520,7 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
       s_len[wave][1][lane] = n.nodes;
       s_len[wave][2][lane] = n.ctx;
     }
+    __builtin_amdgcn_wave_barrier();                  // other lanes read them
     return u;
   };
   auto plan_in_lds = [&](int i) {
