@@ -95,3 +95,24 @@ def test_kernel_timing_counts_the_calls():
         m.kernel_timing_enable(False)
     assert len(kernel) == 3 and min(kernel) > 0
     assert merge[0] > 0 and merge[1] == 0 and merge[2] > 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pages_beyond_32_bit_offsets(dtype):
+    """A cache whose codes pass 4 GiB, its context on the last pages: the bits of the same context in a small cache."""
+    m = d2sd()
+    b = Batch([chain(9), chain(3)], [700, 50], 16, 8, dtype, seed=49)
+    small, n = b.cache, b.cache.num_pages
+    want = [t.clone() for t in b.run()]
+    pages = (1 << 32) // (8 * 1024) + 1000
+    big = m.Kv4Cache(*(torch.empty((pages, *t.shape[1:]), dtype=torch.uint8, device="cuda")
+                       for t in (small.k, small.v, small.k_scale, small.v_scale)))
+    for x, y in ((big.k, small.k), (big.v, small.v), (big.k_scale, small.k_scale), (big.v_scale, small.v_scale)):
+        x[:n] = 255                                    # the same ids without the offset: NaN blocks
+        x[pages - n:] = y
+    b.cache = big
+    b.d[0] = b.d[0] + (pages - n)
+    for kw in ({}, dict(kv_split=128)):
+        out, lse = b.run(**kw)
+        assert torch.equal(out, want[0]) or kw
+        assert torch.isfinite(out.float()).all() and torch.allclose(lse, want[1], atol=1e-5)
