@@ -40,7 +40,8 @@
 // query terms). Tried and slower: V expanded once per workgroup and read back
 // transposed from LDS (545 against 571 of that version, but 246 against 233 with
 // one row tile), the next scores' products ahead of a tile's exponentials (549,
-// spilled), 64-key steps (same), three or four shares per CU (589, 598).
+// spilled), 64-key steps (same), three or four shares per CU (589, 598), eight
+// waves and row tiles on one ring (546 against 548).
 #include <math.h>
 
 #include <type_traits>
