@@ -200,6 +200,13 @@ def _dev(t, name, dtype=None):
     return t.data_ptr()
 
 
+def _here(*tensors):
+    """A call launches on the current device: its tensors have to be there."""
+    for t in tensors:
+        if t.is_cuda and _current_device is not None and t.device.index != _current_device():
+            raise ValueError(f"tensors are on {t.device}, but the current device is cuda:{_current_device()}")
+
+
 def _host_i32(a):
     if type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous:
         return a
@@ -533,6 +540,7 @@ def append_kv4(token_indptr, total_tokens: int, max_tokens: int, k, v, page_tabl
     bfloat16) behind every request's context and advance ctx_len (in place)."""
     code = _rows_code(k, "k", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v", total_tokens, cache.num_kv_heads, k.dtype)
+    _here(k, cache.k)
     i32 = torch.int32
     _check(_append_kv4(ctx_len.numel(), cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
                        page_table.shape[1], max_ctx_len, _dev(token_indptr, "token_indptr", i32), total_tokens,
@@ -546,6 +554,7 @@ def commit_accepted_kv4(B: int, node_indptr, total_nodes: int, path_nodes, accep
     they are written (in place on the cache and on ctx_len)."""
     code = _rows_code(k_tree, "k_tree", k_tree.shape[0], cache.num_kv_heads)
     _rows_code(v_tree, "v_tree", k_tree.shape[0], cache.num_kv_heads, k_tree.dtype)
+    _here(k_tree, cache.k)
     i32 = torch.int32
     _check(_commit_kv4(ctx_len.numel(), B, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
                        page_table.shape[1], max_ctx_len, _dev(node_indptr, "node_indptr", i32), total_nodes,
@@ -563,6 +572,7 @@ def read_kv4(token_indptr, total_tokens: int, max_tokens: int, page_table, cache
     v = v_out if v_out is not None else _empty(stream, shape, k.dtype, cache.k.device)
     code = _rows_code(k, "k_out", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v_out", total_tokens, cache.num_kv_heads, k.dtype)
+    _here(k, cache.k)
     i32 = torch.int32
     _check(_read_kv4(page_table.shape[0], cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
                      page_table.shape[1], _dev(token_indptr, "token_indptr", i32), total_tokens, max_tokens,
@@ -579,6 +589,7 @@ def attn_args_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree, v_tree, node_
     code = {torch.float32: F32, torch.bfloat16: BF16}.get(dt)
     if code is None:
         raise ValueError(f"q dtype {dt} unsupported (float32 or bfloat16)")
+    _here(q, cache.k)
     i32 = torch.int32
     a = AttnArgs(ctx_len.numel(), q.shape[1], cache.num_kv_heads, q.shape[2], PAGE_SIZE, code, stage, sm_scale,
                  total_nodes, max_nodes, max_ctx_len, cache.num_pages, page_table.shape[1],
@@ -643,6 +654,7 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
         raise ValueError(f"logits dtype {logits.dtype} unsupported (float32 or bfloat16)")
     if logits.dim() != 2 or logits.shape[0] < total_nodes:
         raise ValueError(f"logits must be [>= {total_nodes}, vocab], got {tuple(logits.shape)}")
+    _here(logits)
     batch, vocab = node_indptr.numel() - 1, logits.shape[1]
     if out is None:
         out = _empty(stream, logits.shape, logits.dtype, logits.device)

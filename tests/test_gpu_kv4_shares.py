@@ -116,3 +116,20 @@ def test_pages_beyond_32_bit_offsets(dtype):
         out, lse = b.run(**kw)
         assert torch.equal(out, want[0]) or kw
         assert torch.isfinite(out.float()).all() and torch.allclose(lse, want[1], atol=1e-5)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """Before any launch; another device is simulated by what the current one is said to be."""
+    m = d2sd()
+    b = Batch(tokens(2), [40, 20], 4, 1, "bf16", seed=53)
+    one = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    monkeypatch.setattr(m, "_current_device", lambda: 7)
+    x = b.kt[:2]
+    for call in (b.run, lambda: m.append_kv4(one, 2, 1, x, x, b.d[0], b.d[1], b.cache, 40),
+                 lambda: m.commit_accepted_kv4(2, one, 2, one, one, x, x, b.d[0], b.d[1], b.cache, 40),
+                 lambda: m.read_kv4(one, 2, 1, b.d[0], b.cache),
+                 lambda: m.adjust_logits(one, 2, 1, one, b.mask, one, torch.zeros((2, 8), device="cuda"))):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    monkeypatch.undo()
+    b.check(*b.run())
