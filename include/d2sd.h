@@ -581,8 +581,10 @@ d2sd_status d2sd_cascade_workspace_size_kv4(const d2sd_attn_args* args, size_t* 
  * NULL, args->row_group and args->packed 0. kv_split 0 lets the library choose
  * between one workgroup per row group and equal shares of all keys; a multiple
  * of 64 asks for shares of about that many keys. Products are taken with the
- * scales applied exactly and accumulated in fp32. Results do not depend on
- * what else runs, nor on the workspace's contents, and nothing is kept in it.
+ * scales applied exactly and accumulated in fp32; bf16 queries enter with 15
+ * bits below the largest of 32 dims (20 where max_ctx_len <= 512), fp32 ones
+ * with 25. Results do not depend on what else runs, nor on the workspace's
+ * contents, and nothing is kept in it.
  * A tree value that is infinite or NaN reaches the rows that see its node and
  * no other. A row that sees no key gets out = 0, lse = -inf. Errors: as there;
  * UNSUPPORTED also above about 2^28 of (max_ctx_len / 128 + max_nodes / 64 +

@@ -16,8 +16,9 @@
 //    product of the same shape by time in the matrix cores. n terms leave at
 //    most 2^-5n of the block's largest (its next power of two). bf16 queries
 //    are 8 bits long: three terms cut nothing of elements down to 2^-7 of their
-//    block's largest, and 2^-16 of it of smaller ones; with the softmax scale
-//    multiplied in they would need four (565 us instead of 538 for 32 requests
+//    block's largest, and 2^-16 of it of smaller ones, which shows only in the
+//    lse of short contexts: those take a fourth term. With the softmax scale
+//    multiplied in all would need four (565 us instead of 538 for 32 requests
 //    of eight row tiles over 16384 keys), so the scores are scaled instead. fp32
 //    queries take the scale and are held in five terms, 25 bits; their scores'
 //    accumulator starts at -m, so that they leave the product ready for exp2.
@@ -60,18 +61,17 @@ constexpr int kRowBytes = kD * 2;                   // a bf16 row of V in LDS
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x6 __attribute__((ext_vector_type(6)));
 
+// bf16 terms of P, and of tree queries, keys and values.
 template <typename T>
-struct Terms;
-template <>
-struct Terms<__bf16> {
-  static constexpr int Q = 3;   // E2M3 terms of a query
-  static constexpr int P = 1;   // bf16 terms of P, and of tree queries, keys and values
-};
-template <>
-struct Terms<float> {
-  static constexpr int Q = 5;
-  static constexpr int P = 3;
-};
+constexpr int kTerms = sizeof(T) == 4 ? 3 : 1;
+
+// E2M3 terms of a query: five in fp32, three in bf16. What three leave out is
+// the same for all keys, so that its part of an lse is its product with the mean
+// key: relative to the lse 1e-5 with one key, 1.3e-6 with 16, 1.9e-7 with 256,
+// 7.5e-8 with 1024 (normal queries and keys). Calls with contexts up to
+// kFineKeys take a fourth term (7e-8 with one key), which would cost 5% of the
+// time of long contexts and costs 0.2 to 1 us of these (17 to 35 us).
+constexpr int kFineKeys = 512;
 
 // E2M1 keys (32 x 64 dims) by E2M3 query terms; OA, OB: bytes of the scale words.
 template <int OA, int OB>
@@ -496,9 +496,9 @@ struct Copies {
   }
 };
 
-template <typename T>
+template <typename T, int NQ>
 __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 ? 1 : 2))) void kv4_attention_kernel(Kv4Params kp) {
-  constexpr int NQ = Terms<T>::Q, NP = Terms<T>::P;
+  constexpr int NP = kTerms<T>;
   const Params& p = kp.p;
   __shared__ __attribute__((aligned(1024))) char ring[kStages * Tile::BYTES];
   __shared__ float s_m[4][kWave], s_l[4][kWave];
@@ -1014,8 +1014,9 @@ hipError_t launch_kv4_attention(const d2sd_attn_args& a, const d2sd_kv4_cache& c
     e = hipGetLastError();
     if (ev[2]) (void)hipEventRecord(ev[2], stream);
   };
-  if (a.dtype == D2SD_BF16) launch(kv4_attention_kernel<__bf16>, kv4_merge_kernel<__bf16>);
-  else launch(kv4_attention_kernel<float>, kv4_merge_kernel<float>);
+  if (a.dtype != D2SD_BF16) launch(kv4_attention_kernel<float, 5>, kv4_merge_kernel<float>);
+  else if (a.max_ctx_len <= kFineKeys) launch(kv4_attention_kernel<__bf16, 4>, kv4_merge_kernel<__bf16>);
+  else launch(kv4_attention_kernel<__bf16, 3>, kv4_merge_kernel<__bf16>);
   return e;
 }
 

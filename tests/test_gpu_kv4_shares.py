@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from tests.gpu_cases import d2sd
+from tests.kv4_cases import gather
 from tests.test_gpu_kv4_attention import Batch, Rows, canonical, tokens
 
 pytestmark = pytest.mark.gpu
@@ -133,3 +134,29 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
             call()
     monkeypatch.undo()
     b.check(*b.run())
+
+
+@pytest.mark.parametrize("kv_split", [0, 64])
+@pytest.mark.parametrize("ctx", [1, 2, 17, 100, 512])
+def test_lse_of_short_contexts(ctx, kv_split):
+    """bf16 queries over short contexts lose nothing that an lse in 32 bits would show.
+
+    Four E2M3 terms leave at most 2^-20 of the power of two above a block's
+    largest element, itself at most twice that, per element; products and sums
+    are fp32: a score is a sum of 128 products through a chain of at most 16
+    accumulations, the lse one of its keys."""
+    m = d2sd()
+    b = Batch([chain(1)] * 8, [ctx] * 8, 8, 2, "bf16", seed=[54, ctx])
+    _, lse = b.run(stage=m.STAGE_PREFIX, kv_split=kv_split)
+    q, lse = b.q.double().cpu().numpy(), lse.double().cpu().numpy()
+    for r in range(8):
+        k = gather(b.host, "k", b.table[r], 0, ctx)
+        for h in range(8):
+            key = k[:, h // 4]
+            s = key @ q[r, h] / np.sqrt(128.0)
+            want = s.max() + np.log(np.exp(s - s.max()).sum())
+            top = np.abs(q[r, h]).reshape(4, 32).max(1)
+            cut = (2.0 ** -19 * top * np.abs(key).reshape(ctx, 4, 32).sum(2)).sum(1).max() / np.sqrt(128.0)
+            size = (np.abs(key) @ np.abs(q[r, h])).max() / np.sqrt(128.0)
+            tol = cut + 2.0 ** -24 * (18 * size + (ctx + 16) + 4 * abs(want))
+            assert abs(lse[r, h] - want) <= tol, (r, h, lse[r, h] - want, tol)
