@@ -17,11 +17,11 @@
 // Bound by memory: 2 bytes in and 2 out per bf16 logit. Occupancy hides its
 // latency, so the registers of a thread decide: with 8 tokens (64 registers,
 // eight workgroups per CU) 2560 rows of 32000 bf16 logits with 4000 tokens of
-// history take 82.6 us, 4.0 TB/s, where 328 MB at a copy's rate would take 70;
-// 16 tokens (116 registers) took 96.3, and the next row's loads before this one's
-// stores (70 registers) 89.3. 128 or 512 threads: 99.2, 88.4; at most 4 or 12
-// nodes per workgroup: 98.0, 83.4. With 384 rows of 150001 logits, which start
-// at any even address, 56.9 us, 4.1 TB/s.
+// history, 100 biases and 16 masks take 80 us, 4.1 TB/s, where 328 MB at a copy's
+// rate would take 70. Measured at 83: 16 tokens (116 registers) 96, the next
+// row's loads before this one's stores (70 registers) 89, 128 or 512 threads 99
+// and 88, at most 4 or 12 nodes per workgroup 98 and 83. With 384 rows of 150001
+// logits, which start at any even address, 55 us, 4.2 TB/s.
 #include "launchers.h"
 
 namespace d2sd {
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kThr) void adjust_logits_kernel(d2sd_logits_args a,
   __shared__ uint32_t s_head[kThr];
   __shared__ uint32_t s_anc[kMaxPer][kMaskWords];   // ancestor masks of the workgroup's nodes
   __shared__ int s_row[kMaxPer];                    // their token masks
-  __shared__ int s_n, s_before[kThr / kWave];
+  __shared__ int s_n;
 
   int rest = blockIdx.x;
   const int ck = rest % chunks; rest /= chunks;
@@ -180,49 +180,34 @@ __global__ __launch_bounds__(kThr) void adjust_logits_kernel(d2sd_logits_args a,
     counted |= (c & ~kPromptBit ? 1u : 0u) << i;
   }
   if (a.max_bias > 0) {
+    uint32_t* s_owner = s_list;                     // free until the list is made
+    static_assert(kListMax >= kChunk);
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kElems; ++i) s_tok[i * kThr + t] = 0;
+    for (int i = 0; i < kElems; ++i) {
+      s_tok[i * kThr + t] = 0;
+      s_owner[i * kThr + t] = ~0u;
+    }
     __syncthreads();
     const int* tok = a.bias_token + (size_t)b * a.max_bias;
     const float* val = a.bias_value + (size_t)b * a.max_bias;
     const int len = a.bias_len ? clampi(a.bias_len[b], 0, a.max_bias) : a.max_bias;
-    uint32_t* s_bias = s_list;                      // free until the list is made
-    float* s_value = reinterpret_cast<float*>(s_list + kThr);
-    static_assert(kListMax >= 2 * kThr);
-    // kThr entries at a time: those of the chunk are moved together, in order,
-    // and the first of a token adds them all, in order
+    // kThr entries at a time; in a round every token's first entry that is left
+    // adds its value, so that they are summed in order (one round without repeats)
     for (int i0 = 0; i0 < len; i0 += kThr) {
       const int i = i0 + t;
       const uint32_t off = i < len ? (uint32_t)tok[i] - (uint32_t)c0 : ~0u;
       const float value = i < len ? val[i] : 0.0f;
-      const bool in = off < (uint32_t)here;
-      const uint64_t vote = __ballot(in);
-      if (t % kWave == 0) s_before[t / kWave] = __popcll(vote);
-      __syncthreads();
-      int at = __popcll(vote & ((1ull << (t % kWave)) - 1ull)), all = 0;
-#pragma unroll
-      for (int w = 0; w < kThr / kWave; ++w) {
-        if (w < t / kWave) at += s_before[w];
-        all += s_before[w];
-      }
-      if (in) {
-        s_bias[at] = off;
-        s_value[at] = value;
-      }
-      __syncthreads();
-      if (t < all) {
-        const uint32_t mine = s_bias[t];
-        bool first = true;
-        for (int k = 0; k < t && first; ++k) first = s_bias[k] != mine;
-        if (first) {
-          float sum = __uint_as_float(s_tok[mine]);
-          for (int k = t; k < all; ++k)
-            if (s_bias[k] == mine) sum += s_value[k];
-          s_tok[mine] = __float_as_uint(sum);
+      bool left = off < (uint32_t)here;
+      while (__syncthreads_or(left)) {
+        if (left) atomicMin(&s_owner[off], (uint32_t)t);
+        __syncthreads();
+        if (left && s_owner[off] == (uint32_t)t) {
+          s_tok[off] = __float_as_uint(__uint_as_float(s_tok[off]) + value);
+          s_owner[off] = ~0u;
+          left = false;
         }
       }
-      __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < kElems; ++i) add[i] += __uint_as_float(s_tok[i / N * (kThr * N) + t * N + i % N]);

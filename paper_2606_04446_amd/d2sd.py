@@ -187,10 +187,16 @@ def _empty(stream, shape, dtype, device):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _empty_like(stream, t):
+    return torch.empty_like(t) if stream is None else _empty(stream, t.shape, t.dtype, t.device)
+
+
 def _dev(t, name, dtype=None):
     """Device pointer of a contiguous CUDA tensor (None passes NULL)."""
     if t is None:
         return None
+    if t.is_cuda and t.is_contiguous() and (dtype is None or t.dtype is dtype):   # one look for the usual case
+        return t.data_ptr()
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if not t.is_contiguous():
@@ -202,8 +208,11 @@ def _dev(t, name, dtype=None):
 
 def _here(*tensors):
     """A call launches on the current device: its tensors have to be there."""
+    if _current_device is None:
+        return
     for t in tensors:
-        if t.is_cuda and _current_device is not None and t.device.index != _current_device():
+        at = t.get_device()                            # -1: not a device tensor
+        if at >= 0 and at != _current_device():
             raise ValueError(f"tensors are on {t.device}, but the current device is cuda:{_current_device()}")
 
 
@@ -524,11 +533,14 @@ class Kv4Cache:
         return cls(z(HEAD_DIM // 2), z(HEAD_DIM // 2), z(HEAD_DIM // 32), z(HEAD_DIM // 32))
 
 
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def _rows_code(t, name, rows, heads, dtype=None):
     """dtype code of a [rows, heads, 128] tensor."""
-    if tuple(t.shape) != (rows, heads, HEAD_DIM):
+    if t.shape != (rows, heads, HEAD_DIM):
         raise ValueError(f"{name} must have shape ({rows}, {heads}, {HEAD_DIM}), got {tuple(t.shape)}")
-    code = {torch.float32: F32, torch.bfloat16: BF16}.get(t.dtype)
+    code = _CODES.get(t.dtype)
     if code is None or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{name} dtype {t.dtype} unsupported (float32 or bfloat16, K and V alike)")
     return code
@@ -569,7 +581,7 @@ def read_kv4(token_indptr, total_tokens: int, max_tokens: int, page_table, cache
     start[b] + t of request b. Returns (k, v) [total_tokens, kv heads, 128]."""
     shape = (total_tokens, cache.num_kv_heads, HEAD_DIM)
     k = k_out if k_out is not None else _empty(stream, shape, dtype, cache.k.device)
-    v = v_out if v_out is not None else _empty(stream, shape, k.dtype, cache.k.device)
+    v = v_out if v_out is not None else _empty_like(stream, k)
     code = _rows_code(k, "k_out", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v_out", total_tokens, cache.num_kv_heads, k.dtype)
     _here(k, cache.k)
@@ -586,7 +598,7 @@ def attn_args_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree, v_tree, node_
                   sm_scale: float = 0.0, kv_split: int = 0, node_indptr_host=None) -> AttnArgs:
     """attn_args for a context in a 4-bit cache (k_cache and v_cache stay NULL)."""
     dt = q.dtype
-    code = {torch.float32: F32, torch.bfloat16: BF16}.get(dt)
+    code = _CODES.get(dt)
     if code is None:
         raise ValueError(f"q dtype {dt} unsupported (float32 or bfloat16)")
     _here(q, cache.k)
@@ -619,7 +631,7 @@ def cascade_verify_attention_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree
     """Verify attention with the context in a 4-bit cache; returns (out, lse).
     The workspace is allocated when not given."""
     if out is None:
-        out = _empty(stream, q.shape, q.dtype, q.device)
+        out = _empty_like(stream, q)
     if lse is None and want_lse:
         lse = _empty(stream, q.shape[:2], torch.float32, q.device)
     a = attn_args_kv4(q, cache, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, out, lse,
@@ -649,7 +661,7 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
     float32 [batch]; bias_token int32 and bias_value float32 [batch, most] with
     bias_len [batch]; token_mask int32 [masks, ceil(vocab / 32)] with mask_row
     [total_nodes]. Returns out (may be logits; allocated when not given)."""
-    code = {torch.float32: F32, torch.bfloat16: BF16}.get(logits.dtype)
+    code = _CODES.get(logits.dtype)
     if code is None:
         raise ValueError(f"logits dtype {logits.dtype} unsupported (float32 or bfloat16)")
     if logits.dim() != 2 or logits.shape[0] < total_nodes:
@@ -657,7 +669,7 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
     _here(logits)
     batch, vocab = node_indptr.numel() - 1, logits.shape[1]
     if out is None:
-        out = _empty(stream, logits.shape, logits.dtype, logits.device)
+        out = _empty_like(stream, logits)
     if out.shape != logits.shape:
         raise ValueError(f"out must have shape {tuple(logits.shape)}, got {tuple(out.shape)}")
     if token_mask is not None and token_mask.shape[1] != (vocab + 31) // 32:
