@@ -193,12 +193,13 @@ __global__ __launch_bounds__(kThr) void adjust_logits_kernel(d2sd_logits_args a,
     const float* val = a.bias_value + (size_t)b * a.max_bias;
     const int len = a.bias_len ? clampi(a.bias_len[b], 0, a.max_bias) : a.max_bias;
     // kThr entries at a time; in a round every token's first entry that is left
-    // adds its value, so that they are summed in order (one round without repeats)
+    // adds its value, so that they are summed in order: one round without
+    // repeats, and a list that is padded with zeros has none
     for (int i0 = 0; i0 < len; i0 += kThr) {
       const int i = i0 + t;
       const uint32_t off = i < len ? (uint32_t)tok[i] - (uint32_t)c0 : ~0u;
       const float value = i < len ? val[i] : 0.0f;
-      bool left = off < (uint32_t)here;
+      bool left = off < (uint32_t)here && value != 0.0f;
       while (__syncthreads_or(left)) {
         if (left) atomicMin(&s_owner[off], (uint32_t)t);
         __syncthreads();

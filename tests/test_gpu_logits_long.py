@@ -37,3 +37,17 @@ def test_many_requests_are_what_each_is_alone(dtype):
         alone = one.run()
         assert torch.equal(got[s:e], alone)
         one.check(alone)
+
+
+@pytest.mark.parametrize("most", [1, 2, 3, 5, 64, 600])
+def test_bias_lists_that_repeat(most):
+    """Up to `most` entries of a token in a row and far apart, among single ones; a list padded with one id."""
+    b = Batch([build_tree(8, p) for p in ([3, 7], [])], 2500, "f32", seed=[55, most], bias=600, masks=0)
+    rng = np.random.default_rng([56, most])
+    tokens = np.repeat(rng.permutation(2500)[:600], most)[:600]
+    b.kw["bias_token"][0] = tokens
+    b.kw["bias_token"][1] = rng.permutation(tokens)
+    b.kw["bias_token"][1, 200:450] = 7
+    b.kw["bias_value"][1, 300:450] = 0.0
+    b.kw["bias_len"][:] = 600
+    b.check(b.run())
