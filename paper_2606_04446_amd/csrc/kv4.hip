@@ -119,6 +119,36 @@ __global__ __launch_bounds__(kKv4Threads) void advance_kernel(int batch, int max
   ctx_len[b] = C + span_of(token_indptr, b, total, min(max_tokens, max_pages * D2SD_PAGE_SIZE - C)).len;
 }
 
+// Few new rows: one workgroup per request, which then advances ctx_len itself.
+// One launch: a token of 8 heads takes 2.5 us in a graph and 6.5 outside of one,
+// where the two launches with a workgroup per page take 4.4 and 8.8; 128 rows
+// 4.1 and 6.6 against 4.4 and 9.3, 256 rows 5.9 and 6.6 against 4.6 and 9.3, 512
+// rows 9.7 both against 4.7 and 9.3.
+constexpr int kFewThreads = 1024;
+constexpr int kFewRows = 192;
+
+template <typename T>
+__global__ __launch_bounds__(kFewThreads) void append_few_kv4_kernel(
+    int hkv, int num_pages, int max_pages, int max_ctx, const int* __restrict__ token_indptr, int total, int max_tokens,
+    const T* __restrict__ k, const T* __restrict__ v, const int* __restrict__ page_table, int* __restrict__ ctx_len,
+    d2sd_kv4_cache cache) {
+  const int b = blockIdx.x;
+  const int C = clampi(ctx_len[b], 0, max_ctx);
+  const Span s = span_of(token_indptr, b, total, min(max_tokens, max_pages * D2SD_PAGE_SIZE - C));
+  const int sub = threadIdx.x % kRowLanes;
+  for (int r = threadIdx.x / kRowLanes; r < s.len * hkv; r += kFewThreads / kRowLanes) {   // whole rows of lanes
+    const size_t src = ((size_t)s.base * hkv + r) * kKv4Dim + sub * 8;
+    const size_t row = cache_row(page_table + (size_t)b * max_pages, C + r / hkv, num_pages, hkv, r % hkv);
+    float x[8], y[8];
+    load8(k + src, x);
+    load8(v + src, y);
+    write_row8(x, cache.k, cache.k_scale, row, sub);
+    write_row8(y, cache.v, cache.v_scale, row, sub);
+  }
+  __syncthreads();                                  // every thread has read ctx_len[b]
+  if (threadIdx.x == 0) ctx_len[b] = C + s.len;
+}
+
 // One workgroup per request, as a path is at most 64 tokens: ctx_len[b] can
 // then be advanced by the kernel that reads it. A chain of loads (path, page,
 // row) bounds it, not bytes: 32 fp32 paths of up to 16 tokens and 8 heads take
@@ -190,6 +220,17 @@ long long kv4_page_groups(int batch, int max_tokens) { return (long long)batch *
 hipError_t launch_append_kv4(int batch, int hkv, int dtype, int num_pages, int max_pages, int max_ctx,
                              const int* token_indptr, int total, int max_tokens, const void* k, const void* v,
                              const int* page_table, int* ctx_len, const d2sd_kv4_cache& cache, hipStream_t stream) {
+  if ((long long)max_tokens * hkv <= kFewRows) {
+    auto launch = [&](auto kernel, auto* kk, auto* vv) {
+      hipLaunchKernelGGL(kernel, dim3(batch), dim3(kFewThreads), 0, stream, hkv, num_pages, max_pages, max_ctx, token_indptr,
+                         total, max_tokens, kk, vv, page_table, ctx_len, cache);
+    };
+    if (dtype == D2SD_BF16)
+      launch(append_few_kv4_kernel<__bf16>, static_cast<const __bf16*>(k), static_cast<const __bf16*>(v));
+    else
+      launch(append_few_kv4_kernel<float>, static_cast<const float*>(k), static_cast<const float*>(v));
+    return hipGetLastError();
+  }
   const int pages = touched_pages(max_tokens);
   const dim3 grid((unsigned)(batch * (long long)pages), ceil_div(hkv, kHeadsPerGroup));
   auto launch = [&](auto kernel, auto* kk, auto* vv) {

@@ -26,7 +26,8 @@ def attend(**kw):
     assert d2sd._ws_size_kv4(ctypes.byref(a), ctypes.byref(n)) == d2sd.OK
     return d2sd._cascade_kv4(ctypes.byref(a), ctypes.byref(cache), P, n.value, None)
 calls = {
-    "append": (2, lambda: d2sd._append_kv4(2, 2, 128, 16, d2sd.BF16, 64, 32, 100, P, 30, 20, P, P, P, P, ctypes.byref(cache), None)),
+    "append": (2, lambda: d2sd._append_kv4(2, 2, 128, 16, d2sd.BF16, 64, 32, 100, P, 300, 200, P, P, P, P, ctypes.byref(cache), None)),
+    "append, few rows": (1, lambda: d2sd._append_kv4(2, 2, 128, 16, d2sd.BF16, 64, 32, 100, P, 30, 20, P, P, P, P, ctypes.byref(cache), None)),
     "commit": (1, lambda: d2sd._commit_kv4(2, 8, 2, 128, 16, d2sd.BF16, 64, 32, 100, P, 40, P, P, P, P, P, P, ctypes.byref(cache), None)),
     "read": (1, lambda: d2sd._read_kv4(2, 2, 128, 16, d2sd.BF16, 64, 32, P, 30, 20, None, P, ctypes.byref(cache), P, P, None)),
     "attention": (2, attend), "attention, fp32": (2, lambda: attend(dtype=d2sd.F32)),
