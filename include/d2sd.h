@@ -581,10 +581,12 @@ d2sd_status d2sd_cascade_workspace_size_kv4(const d2sd_attn_args* args, size_t* 
  * NULL, args->row_group and args->packed 0. kv_split 0 lets the library choose
  * between one workgroup per row group and equal shares of all keys; a multiple
  * of 64 asks for shares of about that many keys. Products are taken with the
- * scales applied exactly and accumulated in fp32; bf16 queries enter with 15
- * bits below the largest of 32 dims (20 where max_ctx_len <= 512), fp32 ones
- * with 25. Results do not depend on what else runs, nor on the workspace's
- * contents, and nothing is kept in it.
+ * scales applied exactly and accumulated in fp32; a query enters with 20 bits
+ * (bf16) or 25 (fp32) below the power of two above the largest of 32 dims, which
+ * bf16 elements fit into whole down to 2^-12 of it. The softmax's weights are
+ * rounded to bf16 in bf16 calls, as d2sd_cascade_verify_attention's are, and held
+ * in 24 bits in fp32 ones. Results do not depend on what else runs, nor on the
+ * workspace's contents, and nothing is kept in it.
  * A tree value that is infinite or NaN reaches the rows that see its node and
  * no other. A row that sees no key gets out = 0, lse = -inf. Errors: as there;
  * UNSUPPORTED also above about 2^28 of (max_ctx_len / 128 + max_nodes / 64 +
