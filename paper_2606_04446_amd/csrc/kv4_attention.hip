@@ -119,14 +119,17 @@ __device__ __forceinline__ void unpack8(const Raw8<__bf16>& r, float (&v)[8]) {
 }
 
 // v as a sum of bf16 terms, the largest first: each is the rest rounded to bf16.
-template <int N>
+// WIDE: v may be any finite number. Rounding would make one above the largest
+// bf16 infinite, so the first term stops there and the others hold what is left.
+template <int N, bool WIDE = false>
 __device__ __forceinline__ void split_bf16(const float (&v)[8], bf16x8 (&t)[N]) {
+  const float most = __uint_as_float(0x7f7f0000u);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float rest = v[i];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const __bf16 x = (__bf16)rest;
+      const __bf16 x = (__bf16)(WIDE && N > 1 && n == 0 ? __builtin_amdgcn_fmed3f(rest, -most, most) : rest);
       t[n][i] = x;
       rest -= (float)x;
     }
@@ -672,12 +675,12 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
               float v[8];
               unpack8(rq8[i], v);
               bf16x8 tq[NP];
-              split_bf16<NP>(v, tq);
+              split_bf16<NP, true>(v, tq);
 #pragma unroll
               for (int kb = 0; kb < 2; ++kb) {
                 unpack8(rk8[kb][i], v);
                 bf16x8 tk[NP];
-                split_bf16<NP>(v, tk);
+                split_bf16<NP, true>(v, tk);
 #pragma unroll
                 for (int x = NP - 1; x >= 0; --x)     // products below the last term are left out
 #pragma unroll
@@ -717,7 +720,7 @@ __global__ __launch_bounds__(4 * kWave) __attribute__((amdgpu_waves_per_eu(sizeo
               }
             if (wild) s_flag = 1;
             bf16x8 t[NP];
-            split_bf16<NP>(v, t);
+            split_bf16<NP, true>(v, t);
             *reinterpret_cast<bf16x8*>(tree_v + chunk_at(row, c)) = t[n];
           }
           lds_barrier();
