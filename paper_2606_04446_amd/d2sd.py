@@ -546,6 +546,18 @@ def _rows_code(t, name, rows, heads, dtype=None):
     return code
 
 
+def _entries(t, name, n):
+    if t.numel() < n:
+        raise ValueError(f"{name} must have {n} entries, got {t.numel()}")
+
+
+def _pages_of(page_table, batch):
+    """Row length of a page table that has to have a row for each of `batch` requests."""
+    if page_table.dim() != 2 or page_table.size(0) < batch:
+        raise ValueError(f"page_table must be [>= {batch}, pages], got {tuple(page_table.shape)}")
+    return page_table.size(1)
+
+
 def append_kv4(token_indptr, total_tokens: int, max_tokens: int, k, v, page_table, ctx_len, cache: Kv4Cache,
                max_ctx_len: int, stream=None):
     """Quantise new tokens' K/V [total_tokens, kv heads, 128] (float32 or
@@ -578,16 +590,20 @@ def commit_accepted_kv4(B: int, node_indptr, total_nodes: int, path_nodes, accep
 def read_kv4(token_indptr, total_tokens: int, max_tokens: int, page_table, cache: Kv4Cache, start=None,
              dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
     """The values a 4-bit cache stands for: row token_indptr[b] + t is position
-    start[b] + t of request b. Returns (k, v) [total_tokens, kv heads, 128]."""
+    start[b] + t of request b, for the requests that token_indptr [batch + 1]
+    counts. Returns (k, v) [total_tokens, kv heads, 128]."""
     shape = (total_tokens, cache.num_kv_heads, HEAD_DIM)
     k = k_out if k_out is not None else _empty(stream, shape, dtype, cache.k.device)
     v = v_out if v_out is not None else _empty_like(stream, k)
     code = _rows_code(k, "k_out", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v_out", total_tokens, cache.num_kv_heads, k.dtype)
     _here(k, cache.k)
-    i32 = torch.int32
-    _check(_read_kv4(page_table.shape[0], cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
-                     page_table.shape[1], _dev(token_indptr, "token_indptr", i32), total_tokens, max_tokens,
+    i32, batch = torch.int32, token_indptr.numel() - 1
+    max_pages = _pages_of(page_table, batch)
+    if start is not None:
+        _entries(start, "start", batch)
+    _check(_read_kv4(batch, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
+                     max_pages, _dev(token_indptr, "token_indptr", i32), total_tokens, max_tokens,
                      _dev(start, "start", i32), _dev(page_table, "page_table", i32), cache.pointers, _dev(k, "k_out"),
                      _dev(v, "v_out"), _stream(stream)), "d2sd_read_kv4")
     return k, v

@@ -1,0 +1,80 @@
+"""What the binding of the 4-bit cache refuses, and what it hands to the library:
+device tensors are stood in for by their sizes, and the library by a recorder, so
+that nothing is launched."""
+
+import pytest
+import torch
+
+from paper_2606_04446_amd import d2sd
+
+I32, U8, BF16, F32 = torch.int32, torch.uint8, torch.bfloat16, torch.float32
+
+
+class Tensor:
+    """A contiguous device tensor without data."""
+
+    is_cuda = True
+
+    def __init__(self, *shape, dtype=I32, at=0):
+        self.shape, self.dtype, self.at = torch.Size(shape), dtype, at
+        self.device = torch.device("cuda", at)
+
+    def get_device(self):
+        return self.at
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return self.shape.numel()
+
+    def element_size(self):
+        return torch.empty((), dtype=self.dtype).element_size()
+
+    def dim(self):
+        return len(self.shape)
+
+    def size(self, i):
+        return self.shape[i]
+
+    def data_ptr(self):
+        return 1 << 20
+
+
+def cache(pages=9, heads=2, at=0):
+    k = lambda n: Tensor(pages, heads, 16, n, dtype=U8, at=at)
+    return d2sd.Kv4Cache(k(64), k(64), k(4), k(4))
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Arguments of the library calls that get through."""
+    got = []
+    for name in ("_append_kv4", "_commit_kv4", "_read_kv4", "_cascade_kv4", "_ws_size_kv4", "_adjust"):
+        monkeypatch.setattr(d2sd, name, lambda *a: got.append(a) or d2sd.OK)
+    monkeypatch.setattr(d2sd, "_current_device", lambda: 0)
+    monkeypatch.setattr(d2sd, "_stream", lambda s: 0)
+    return got
+
+
+def read(**kw):
+    a = dict(token_indptr=Tensor(4), total_tokens=20, max_tokens=9, page_table=Tensor(3, 5), cache=cache(), start=None,
+             k_out=Tensor(20, 2, 128, dtype=BF16), v_out=Tensor(20, 2, 128, dtype=BF16))
+    return d2sd.read_kv4(**{**a, **kw})
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(page_table=Tensor(8, 5)), dict(start=Tensor(3)), dict(start=Tensor(8))])
+def test_read_counts_the_requests_by_their_offsets(calls, kw):
+    """A page table with rows to spare asks for no more requests than token_indptr has."""
+    read(**kw)
+    assert len(calls) == 1 and calls[0][0] == 3 and calls[0][6] == 5
+
+
+@pytest.mark.parametrize("kw, what", [
+    (dict(page_table=Tensor(2, 5)), "page_table"), (dict(page_table=Tensor(15)), "page_table"),
+    (dict(start=Tensor(2)), "start"), (dict(k_out=Tensor(19, 2, 128, dtype=BF16)), "k_out"),
+    (dict(v_out=Tensor(20, 1, 128, dtype=BF16)), "v_out"), (dict(v_out=Tensor(20, 2, 128, dtype=F32)), "v_out")])
+def test_read_refuses_short_tensors(calls, kw, what):
+    with pytest.raises(ValueError, match=what):
+        read(**kw)
+    assert not calls
