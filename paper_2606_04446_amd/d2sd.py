@@ -565,9 +565,11 @@ def append_kv4(token_indptr, total_tokens: int, max_tokens: int, k, v, page_tabl
     code = _rows_code(k, "k", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v", total_tokens, cache.num_kv_heads, k.dtype)
     _here(k, cache.k)
-    i32 = torch.int32
-    _check(_append_kv4(ctx_len.numel(), cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
-                       page_table.shape[1], max_ctx_len, _dev(token_indptr, "token_indptr", i32), total_tokens,
+    i32, batch = torch.int32, ctx_len.numel()
+    max_pages = _pages_of(page_table, batch)
+    _entries(token_indptr, "token_indptr", batch + 1)
+    _check(_append_kv4(batch, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
+                       max_pages, max_ctx_len, _dev(token_indptr, "token_indptr", i32), total_tokens,
                        max_tokens, _dev(k, "k"), _dev(v, "v"), _dev(page_table, "page_table", i32),
                        _dev(ctx_len, "ctx_len", i32), cache.pointers, _stream(stream)), "d2sd_append_kv4")
 

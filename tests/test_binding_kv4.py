@@ -78,3 +78,25 @@ def test_read_refuses_short_tensors(calls, kw, what):
     with pytest.raises(ValueError, match=what):
         read(**kw)
     assert not calls
+
+
+def append(**kw):
+    a = dict(token_indptr=Tensor(4), total_tokens=20, max_tokens=9, k=Tensor(20, 2, 128, dtype=BF16),
+             v=Tensor(20, 2, 128, dtype=BF16), page_table=Tensor(3, 5), ctx_len=Tensor(3), cache=cache(), max_ctx_len=70)
+    return d2sd.append_kv4(**{**a, **kw})
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(page_table=Tensor(8, 5)), dict(token_indptr=Tensor(9))])
+def test_append_takes_longer_tensors(calls, kw):
+    append(**kw)
+    assert len(calls) == 1 and calls[0][0] == 3 and calls[0][6] == 5
+
+
+@pytest.mark.parametrize("kw, what", [
+    (dict(token_indptr=Tensor(3)), "token_indptr"), (dict(page_table=Tensor(2, 5)), "page_table"),
+    (dict(page_table=Tensor(15)), "page_table"), (dict(k=Tensor(19, 2, 128, dtype=BF16)), "k must"),
+    (dict(v=Tensor(20, 2, 64, dtype=BF16)), "v must"), (dict(v=Tensor(20, 2, 128, dtype=F32)), "v dtype")])
+def test_append_refuses_short_tensors(calls, kw, what):
+    with pytest.raises(ValueError, match=what):
+        append(**kw)
+    assert not calls
