@@ -558,6 +558,14 @@ def _pages_of(page_table, batch):
     return page_table.size(1)
 
 
+def _rows_from(t, name, rows, heads, dtype):
+    """A [>= rows, heads, 128] tensor of that dtype."""
+    if t.dim() != 3 or t.size(0) < rows or t.size(1) != heads or t.size(2) != HEAD_DIM:
+        raise ValueError(f"{name} must be [>= {rows}, {heads}, {HEAD_DIM}], got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+
+
 def append_kv4(token_indptr, total_tokens: int, max_tokens: int, k, v, page_table, ctx_len, cache: Kv4Cache,
                max_ctx_len: int, stream=None):
     """Quantise new tokens' K/V [total_tokens, kv heads, 128] (float32 or
@@ -578,12 +586,21 @@ def commit_accepted_kv4(B: int, node_indptr, total_nodes: int, path_nodes, accep
                         ctx_len, cache: Kv4Cache, max_ctx_len: int, stream=None):
     """commit_accepted_kv for a 4-bit cache: the accepted rows are quantised as
     they are written (in place on the cache and on ctx_len)."""
-    code = _rows_code(k_tree, "k_tree", k_tree.shape[0], cache.num_kv_heads)
-    _rows_code(v_tree, "v_tree", k_tree.shape[0], cache.num_kv_heads, k_tree.dtype)
+    code = _CODES.get(k_tree.dtype)
+    if code is None:
+        raise ValueError(f"k_tree dtype {k_tree.dtype} unsupported (float32 or bfloat16)")
     _here(k_tree, cache.k)
-    i32 = torch.int32
-    _check(_commit_kv4(ctx_len.numel(), B, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
-                       page_table.shape[1], max_ctx_len, _dev(node_indptr, "node_indptr", i32), total_nodes,
+    _rows_from(k_tree, "k_tree", total_nodes, cache.num_kv_heads, k_tree.dtype)
+    _rows_from(v_tree, "v_tree", total_nodes, cache.num_kv_heads, k_tree.dtype)
+    i32, batch = torch.int32, ctx_len.numel()
+    max_pages = _pages_of(page_table, batch)
+    _entries(node_indptr, "node_indptr", batch + 1)
+    _entries(path_nodes, "path_nodes", batch * B)
+    if batch > 1 and path_nodes.dim() == 2 and path_nodes.size(1) != B:
+        raise ValueError(f"path_nodes must be [{batch}, {B}], got {tuple(path_nodes.shape)}")
+    _entries(accept_len, "accept_len", batch)
+    _check(_commit_kv4(batch, B, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
+                       max_pages, max_ctx_len, _dev(node_indptr, "node_indptr", i32), total_nodes,
                        _dev(path_nodes, "path_nodes", i32), _dev(accept_len, "accept_len", i32),
                        _dev(k_tree, "k_tree"), _dev(v_tree, "v_tree"), _dev(page_table, "page_table", i32),
                        _dev(ctx_len, "ctx_len", i32), cache.pointers, _stream(stream)), "d2sd_commit_accepted_kv4")

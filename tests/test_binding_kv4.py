@@ -100,3 +100,31 @@ def test_append_refuses_short_tensors(calls, kw, what):
     with pytest.raises(ValueError, match=what):
         append(**kw)
     assert not calls
+
+
+def commit(**kw):
+    a = dict(B=4, node_indptr=Tensor(4), total_nodes=20, path_nodes=Tensor(3, 4), accept_len=Tensor(3),
+             k_tree=Tensor(20, 2, 128, dtype=F32), v_tree=Tensor(20, 2, 128, dtype=F32), page_table=Tensor(3, 5),
+             ctx_len=Tensor(3), cache=cache(), max_ctx_len=70)
+    return d2sd.commit_accepted_kv4(**{**a, **kw})
+
+
+@pytest.mark.parametrize("kw", [
+    dict(), dict(page_table=Tensor(8, 5)), dict(node_indptr=Tensor(9)), dict(accept_len=Tensor(4)), dict(path_nodes=Tensor(6, 4)),
+    dict(k_tree=Tensor(32, 2, 128, dtype=F32)), dict(v_tree=Tensor(21, 2, 128, dtype=F32))])
+def test_commit_takes_longer_tensors(calls, kw):
+    """As a captured step's buffers are."""
+    commit(**kw)
+    assert len(calls) == 1 and calls[0][0] == 3 and calls[0][7] == 5 and calls[0][10] == 20
+
+
+@pytest.mark.parametrize("kw, what", [
+    (dict(node_indptr=Tensor(3)), "node_indptr"), (dict(page_table=Tensor(2, 5)), "page_table"),
+    (dict(path_nodes=Tensor(3, 3)), "path_nodes"), (dict(path_nodes=Tensor(3, 5)), "path_nodes"), (dict(accept_len=Tensor(2)), "accept_len"),
+    (dict(k_tree=Tensor(19, 2, 128, dtype=F32)), "k_tree"), (dict(k_tree=Tensor(20, 8, 128, dtype=F32)), "k_tree"),
+    (dict(v_tree=Tensor(19, 2, 128, dtype=F32)), "v_tree"), (dict(v_tree=Tensor(20, 2, 64, dtype=F32)), "v_tree"),
+    (dict(v_tree=Tensor(20, 2, 128, dtype=BF16)), "v_tree"), (dict(k_tree=Tensor(20, 2, 128, dtype=torch.float16)), "k_tree")])
+def test_commit_refuses_short_tensors(calls, kw, what):
+    with pytest.raises(ValueError, match=what):
+        commit(**kw)
+    assert not calls
