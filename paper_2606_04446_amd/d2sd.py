@@ -637,9 +637,20 @@ def attn_args_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree, v_tree, node_
     if code is None:
         raise ValueError(f"q dtype {dt} unsupported (float32 or bfloat16)")
     _here(q, cache.k)
-    i32 = torch.int32
-    a = AttnArgs(ctx_len.numel(), q.shape[1], cache.num_kv_heads, q.shape[2], PAGE_SIZE, code, stage, sm_scale,
-                 total_nodes, max_nodes, max_ctx_len, cache.num_pages, page_table.shape[1],
+    i32, batch, heads = torch.int32, ctx_len.numel(), q.size(1)
+    _rows_from(q, "q", total_nodes, heads, dt)
+    _rows_from(out, "out", total_nodes, heads, dt)
+    if lse is not None:
+        _entries(lse, "lse", total_nodes * heads)
+    max_pages = _pages_of(page_table, batch)
+    _entries(node_indptr, "node_indptr", batch + 1)
+    if stage != STAGE_PREFIX:                          # which reads none of the tree's own
+        _rows_from(k_tree, "k_tree", total_nodes, cache.num_kv_heads, dt)
+        _rows_from(v_tree, "v_tree", total_nodes, cache.num_kv_heads, dt)
+        if anc_mask is not None and anc_mask.size(0) < total_nodes:
+            raise ValueError(f"anc_mask must be [>= {total_nodes}, words], got {tuple(anc_mask.shape)}")
+    a = AttnArgs(batch, heads, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, stage, sm_scale,
+                 total_nodes, max_nodes, max_ctx_len, cache.num_pages, max_pages,
                  anc_mask.shape[1] if anc_mask is not None else 0, kv_split, 0, 0, _dev(q, "q", dt), None, None,
                  _dev(page_table, "page_table", i32), _dev(ctx_len, "ctx_len", i32), _dev(k_tree, "k_tree", dt),
                  _dev(v_tree, "v_tree", dt), _dev(node_indptr, "node_indptr", i32), _dev(anc_mask, "anc_mask", i32),

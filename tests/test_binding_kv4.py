@@ -128,3 +128,39 @@ def test_commit_refuses_short_tensors(calls, kw, what):
     with pytest.raises(ValueError, match=what):
         commit(**kw)
     assert not calls
+
+
+def attend(**kw):
+    a = dict(q=Tensor(20, 8, 128, dtype=BF16), cache=cache(), page_table=Tensor(3, 5), ctx_len=Tensor(3),
+             k_tree=Tensor(20, 2, 128, dtype=BF16), v_tree=Tensor(20, 2, 128, dtype=BF16), node_indptr=Tensor(4),
+             anc_mask=Tensor(20, 1), total_nodes=20, max_nodes=9, max_ctx_len=70, out=Tensor(20, 8, 128, dtype=BF16),
+             lse=Tensor(20, 8, dtype=F32), workspace=Tensor(64, dtype=U8))
+    return d2sd.cascade_verify_attention_kv4(**{**a, **kw})
+
+
+@pytest.mark.parametrize("kw", [
+    dict(), dict(page_table=Tensor(8, 5)), dict(node_indptr=Tensor(9)), dict(q=Tensor(32, 8, 128, dtype=BF16)),
+    dict(k_tree=Tensor(32, 2, 128, dtype=BF16)), dict(v_tree=Tensor(21, 2, 128, dtype=BF16)), dict(anc_mask=Tensor(32, 1)),
+    dict(out=Tensor(32, 8, 128, dtype=BF16)), dict(lse=Tensor(400, dtype=F32)), dict(lse=None, want_lse=False),
+    dict(stage=d2sd.STAGE_PREFIX, k_tree=Tensor(1, dtype=BF16), v_tree=Tensor(1, dtype=BF16), anc_mask=None)])
+def test_attention_takes_longer_tensors(calls, kw):
+    attend(**kw)
+    a = calls[0][0]._obj
+    assert len(calls) == 1 and (a.batch, a.num_qo_heads, a.num_kv_heads, a.max_pages, a.total_nodes) == (3, 8, 2, 5, 20)
+
+
+@pytest.mark.parametrize("kw, what", [
+    (dict(q=Tensor(19, 8, 128, dtype=BF16)), "q must"), (dict(q=Tensor(20, 8, 64, dtype=BF16)), "q must"),
+    (dict(q=Tensor(20, 8, 128, dtype=torch.float16)), "q dtype"),
+    (dict(out=Tensor(19, 8, 128, dtype=BF16)), "out"), (dict(out=Tensor(20, 4, 128, dtype=BF16)), "out"),
+    (dict(out=Tensor(20, 8, 128, dtype=F32)), "out"), (dict(lse=Tensor(20, 4, dtype=F32)), "lse"),
+    (dict(lse=Tensor(20, 8, dtype=BF16)), "lse"), (dict(k_tree=Tensor(19, 2, 128, dtype=BF16)), "k_tree"),
+    (dict(k_tree=Tensor(20, 8, 128, dtype=BF16)), "k_tree"), (dict(v_tree=Tensor(20, 1, 128, dtype=BF16)), "v_tree"),
+    (dict(v_tree=Tensor(20, 2, 128, dtype=F32)), "v_tree"), (dict(page_table=Tensor(2, 5)), "page_table"),
+    (dict(node_indptr=Tensor(3)), "node_indptr"), (dict(anc_mask=Tensor(19, 1)), "anc_mask"),
+    (dict(stage=d2sd.STAGE_TREE, anc_mask=Tensor(19, 1)), "anc_mask"),
+    (dict(stage=d2sd.STAGE_PREFIX, q=Tensor(19, 8, 128, dtype=BF16)), "q must")])
+def test_attention_refuses_short_tensors(calls, kw, what):
+    with pytest.raises(ValueError, match=what):
+        attend(**kw)
+    assert not calls
