@@ -207,13 +207,13 @@ def _dev(t, name, dtype=None):
 
 
 def _here(*tensors):
-    """A call launches on the current device: its tensors have to be there."""
+    """A call launches on the current device: its tensors (None: not given) have to be there."""
     if _current_device is None:
         return
+    here = _current_device()
     for t in tensors:
-        at = t.get_device()                            # -1: not a device tensor
-        if at >= 0 and at != _current_device():
-            raise ValueError(f"tensors are on {t.device}, but the current device is cuda:{_current_device()}")
+        if t is not None and t.get_device() != here and t.is_cuda:   # others are refused for that
+            raise ValueError(f"tensors are on {t.device}, but the current device is cuda:{here}")
 
 
 def _host_i32(a):
@@ -572,7 +572,7 @@ def append_kv4(token_indptr, total_tokens: int, max_tokens: int, k, v, page_tabl
     bfloat16) behind every request's context and advance ctx_len (in place)."""
     code = _rows_code(k, "k", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v", total_tokens, cache.num_kv_heads, k.dtype)
-    _here(k, cache.k)
+    _here(k, v, token_indptr, page_table, ctx_len, cache.k)
     i32, batch = torch.int32, ctx_len.numel()
     max_pages = _pages_of(page_table, batch)
     _entries(token_indptr, "token_indptr", batch + 1)
@@ -589,7 +589,7 @@ def commit_accepted_kv4(B: int, node_indptr, total_nodes: int, path_nodes, accep
     code = _CODES.get(k_tree.dtype)
     if code is None:
         raise ValueError(f"k_tree dtype {k_tree.dtype} unsupported (float32 or bfloat16)")
-    _here(k_tree, cache.k)
+    _here(k_tree, v_tree, node_indptr, path_nodes, accept_len, page_table, ctx_len, cache.k)
     _rows_from(k_tree, "k_tree", total_nodes, cache.num_kv_heads, k_tree.dtype)
     _rows_from(v_tree, "v_tree", total_nodes, cache.num_kv_heads, k_tree.dtype)
     i32, batch = torch.int32, ctx_len.numel()
@@ -616,7 +616,7 @@ def read_kv4(token_indptr, total_tokens: int, max_tokens: int, page_table, cache
     v = v_out if v_out is not None else _empty_like(stream, k)
     code = _rows_code(k, "k_out", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v_out", total_tokens, cache.num_kv_heads, k.dtype)
-    _here(k, cache.k)
+    _here(k, v, token_indptr, start, page_table, cache.k)
     i32, batch = torch.int32, token_indptr.numel() - 1
     max_pages = _pages_of(page_table, batch)
     if start is not None:
@@ -636,7 +636,7 @@ def attn_args_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree, v_tree, node_
     code = _CODES.get(dt)
     if code is None:
         raise ValueError(f"q dtype {dt} unsupported (float32 or bfloat16)")
-    _here(q, cache.k)
+    _here(q, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, out, lse, cache.k)
     i32, batch, heads = torch.int32, ctx_len.numel(), q.size(1)
     _rows_from(q, "q", total_nodes, heads, dt)
     _rows_from(out, "out", total_nodes, heads, dt)
@@ -683,10 +683,12 @@ def cascade_verify_attention_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree
     a = attn_args_kv4(q, cache, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, out, lse,
                       total_nodes=total_nodes, max_nodes=max_nodes, max_ctx_len=max_ctx_len, stage=stage,
                       sm_scale=sm_scale, kv_split=kv_split, node_indptr_host=node_indptr_host)
-    if workspace is None:      # a given one is checked against the call's need by the library
+    if workspace is None:      # a given one's size is checked against the call's need by the library
         need = cascade_workspace_size_kv4(a)
         if need > 0:
             workspace = _empty(stream, need, torch.uint8, q.device)
+    else:
+        _here(workspace)
     ws_ptr = _dev(workspace, "workspace") if workspace is not None else None
     ws_len = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_cascade_kv4(ctypes.byref(a), cache.pointers, ws_ptr, ws_len, _stream(stream)),
@@ -712,7 +714,8 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
         raise ValueError(f"logits dtype {logits.dtype} unsupported (float32 or bfloat16)")
     if logits.dim() != 2 or logits.shape[0] < total_nodes:
         raise ValueError(f"logits must be [>= {total_nodes}, vocab], got {tuple(logits.shape)}")
-    _here(logits)
+    _here(logits, node_indptr, depth, anc_mask, draft_tokens, history, history_len, prompt_len, repetition, presence, frequency,
+          bias_token, bias_value, bias_len, token_mask, mask_row, out)
     batch, vocab = node_indptr.numel() - 1, logits.shape[1]
     if out is None:
         out = _empty_like(stream, logits)

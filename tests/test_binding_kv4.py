@@ -164,3 +164,48 @@ def test_attention_refuses_short_tensors(calls, kw, what):
     with pytest.raises(ValueError, match=what):
         attend(**kw)
     assert not calls
+
+
+def adjust(**kw):
+    i, f = Tensor(3), Tensor(3, dtype=F32)
+    a = dict(node_indptr=Tensor(4), total_nodes=20, max_nodes=9, depth=Tensor(20), anc_mask=Tensor(20, 1), draft_tokens=Tensor(20),
+             logits=Tensor(20, 100, dtype=F32), history=Tensor(3, 7), history_len=i, prompt_len=i, repetition=f, presence=f,
+             frequency=f, bias_token=Tensor(3, 2), bias_value=Tensor(3, 2, dtype=F32), bias_len=i, token_mask=Tensor(5, 4),
+             mask_row=Tensor(20), out=Tensor(20, 100, dtype=F32))
+    a = {**a, **kw}
+    first = [a.pop(n) for n in ("node_indptr", "total_nodes", "max_nodes", "depth", "anc_mask", "draft_tokens", "logits")]
+    return d2sd.adjust_logits(*first, **a)
+
+
+CALLS = {"append": append, "commit": commit, "read": read, "attend": attend, "adjust": adjust}
+
+
+@pytest.mark.parametrize("call, name, shape, dtype", [
+    (call, name, shape, dtype) for call, names in {
+        "append": [("token_indptr", (4,), I32), ("k", (20, 2, 128), BF16), ("v", (20, 2, 128), BF16), ("page_table", (3, 5), I32),
+                   ("ctx_len", (3,), I32)],
+        "commit": [("node_indptr", (4,), I32), ("path_nodes", (3, 4), I32), ("accept_len", (3,), I32), ("k_tree", (20, 2, 128), F32),
+                   ("v_tree", (20, 2, 128), F32), ("page_table", (3, 5), I32), ("ctx_len", (3,), I32)],
+        "read": [("token_indptr", (4,), I32), ("start", (3,), I32), ("page_table", (3, 5), I32), ("k_out", (20, 2, 128), BF16),
+                 ("v_out", (20, 2, 128), BF16)],
+        "attend": [("q", (20, 8, 128), BF16), ("page_table", (3, 5), I32), ("ctx_len", (3,), I32), ("k_tree", (20, 2, 128), BF16),
+                   ("v_tree", (20, 2, 128), BF16), ("node_indptr", (4,), I32), ("anc_mask", (20, 1), I32),
+                   ("out", (20, 8, 128), BF16), ("lse", (20, 8), F32), ("workspace", (64,), U8)],
+        "adjust": [("node_indptr", (4,), I32), ("depth", (20,), I32), ("anc_mask", (20, 1), I32), ("draft_tokens", (20,), I32),
+                   ("logits", (20, 100), F32), ("history", (3, 7), I32), ("history_len", (3,), I32), ("prompt_len", (3,), I32),
+                   ("repetition", (3,), F32), ("presence", (3,), F32), ("frequency", (3,), F32), ("bias_token", (3, 2), I32),
+                   ("bias_value", (3, 2), F32), ("bias_len", (3,), I32), ("token_mask", (5, 4), I32), ("mask_row", (20,), I32),
+                   ("out", (20, 100), F32)]}.items() for name, shape, dtype in names])
+def test_a_tensor_of_another_device_is_refused(calls, call, name, shape, dtype):
+    with pytest.raises(ValueError, match="current device"):
+        CALLS[call](**{name: Tensor(*shape, dtype=dtype, at=1)})
+    assert not calls
+    CALLS[call]()
+    assert len(calls) == 1
+
+
+@pytest.mark.parametrize("call", ["append", "commit", "read", "attend"])
+def test_a_cache_of_another_device_is_refused(calls, call):
+    with pytest.raises(ValueError, match="current device"):
+        CALLS[call](cache=cache(at=1))
+    assert not calls
