@@ -721,8 +721,10 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
         out = _empty_like(stream, logits)
     if out.shape != logits.shape:
         raise ValueError(f"out must have shape {tuple(logits.shape)}, got {tuple(out.shape)}")
-    if token_mask is not None and token_mask.shape[1] != (vocab + 31) // 32:
-        raise ValueError(f"token_mask must have {(vocab + 31) // 32} words a row, got {token_mask.shape[1]}")
+    if anc_mask.dim() != 2 or anc_mask.size(0) < total_nodes:
+        raise ValueError(f"anc_mask must be [>= {total_nodes}, words], got {tuple(anc_mask.shape)}")
+    if token_mask is not None and (token_mask.dim() != 2 or token_mask.size(1) != (vocab + 31) // 32):
+        raise ValueError(f"token_mask must be [masks, {(vocab + 31) // 32}], got {tuple(token_mask.shape)}")
     for t, name, n in ((depth, "depth", total_nodes), (draft_tokens, "draft_tokens", total_nodes),
                        (mask_row, "mask_row", total_nodes), (history_len, "history_len", batch),
                        (prompt_len, "prompt_len", batch), (repetition, "repetition", batch),

@@ -209,3 +209,26 @@ def test_a_cache_of_another_device_is_refused(calls, call):
     with pytest.raises(ValueError, match="current device"):
         CALLS[call](cache=cache(at=1))
     assert not calls
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(anc_mask=Tensor(32, 1)), dict(depth=Tensor(32)), dict(mask_row=Tensor(21)),
+                                dict(logits=Tensor(24, 100, dtype=F32), out=Tensor(24, 100, dtype=F32))])
+def test_adjust_takes_longer_tensors(calls, kw):
+    adjust(**kw)
+    a = calls[0][0]._obj
+    assert len(calls) == 1 and (a.batch, a.total_nodes, a.vocab, a.num_masks, a.max_history) == (3, 20, 100, 5, 7)
+
+
+@pytest.mark.parametrize("kw, what", [
+    (dict(anc_mask=Tensor(19, 1)), "anc_mask"), (dict(anc_mask=Tensor(20)), "anc_mask"), (dict(depth=Tensor(19)), "depth"),
+    (dict(draft_tokens=Tensor(19)), "draft_tokens"), (dict(mask_row=Tensor(19)), "mask_row"), (dict(token_mask=Tensor(5, 3)), "token_mask"),
+    (dict(token_mask=Tensor(20)), "token_mask"), (dict(history=Tensor(2, 7)), "history"), (dict(history_len=Tensor(2)), "history_len"),
+    (dict(prompt_len=Tensor(2)), "prompt_len"), (dict(repetition=Tensor(2, dtype=F32)), "repetition"),
+    (dict(presence=Tensor(2, dtype=F32)), "presence"), (dict(frequency=Tensor(2, dtype=F32)), "frequency"),
+    (dict(bias_len=Tensor(2)), "bias_len"), (dict(bias_value=Tensor(3, 1, dtype=F32)), "bias_value"), (dict(bias_value=None), "bias_value"),
+    (dict(bias_token=Tensor(2, 2)), "bias_token"), (dict(logits=Tensor(19, 100, dtype=F32)), "logits"),
+    (dict(out=Tensor(20, 99, dtype=F32)), "out"), (dict(out=Tensor(20, 100, dtype=BF16)), "out")])
+def test_adjust_refuses_short_tensors(calls, kw, what):
+    with pytest.raises(ValueError, match=what):
+        adjust(**kw)
+    assert not calls
