@@ -191,14 +191,17 @@ def _empty_like(stream, t):
     return torch.empty_like(t) if stream is None else _empty(stream, t.shape, t.dtype, t.device)
 
 
-def _dev(t, name, dtype=None):
-    """Device pointer of a contiguous CUDA tensor (None passes NULL)."""
+def _dev(t, name, dtype=None, here=None):
+    """Device pointer of a contiguous CUDA tensor (None passes NULL), on device `here` where it is given."""
     if t is None:
         return None
-    if t.is_cuda and t.is_contiguous() and (dtype is None or t.dtype is dtype):   # one look for the usual case
+    # one look for the usual case
+    if (t.is_cuda if here is None else t.get_device() == here) and t.is_contiguous() and (dtype is None or t.dtype is dtype):
         return t.data_ptr()
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    if here is not None and t.get_device() != here:
+        raise ValueError(f"{name} is on {t.device}, but the current device is cuda:{here}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     if dtype is not None and t.dtype != dtype:
@@ -206,14 +209,9 @@ def _dev(t, name, dtype=None):
     return t.data_ptr()
 
 
-def _here(*tensors):
-    """A call launches on the current device: its tensors (None: not given) have to be there."""
-    if _current_device is None:
-        return
-    here = _current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != here and t.is_cuda:   # others are refused for that
-            raise ValueError(f"tensors are on {t.device}, but the current device is cuda:{here}")
+def _here():
+    """Index of the current device, on which a call launches and its tensors have to be."""
+    return _current_device() if _current_device is not None else None
 
 
 def _host_i32(a):
@@ -524,7 +522,7 @@ class Kv4Cache:
         self.pointers = Kv4Pointers(_dev(k, "k", u8), _dev(v, "v", u8), _dev(k_scale, "k_scale", u8),
                                     _dev(v_scale, "v_scale", u8))
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.num_pages, self.num_kv_heads = k.shape[0], k.shape[1]
+        self.num_pages, self.num_kv_heads, self.device_index = k.shape[0], k.shape[1], k.get_device()
 
     @classmethod
     def empty(cls, num_pages: int, num_kv_heads: int, device="cuda"):
@@ -553,17 +551,22 @@ def _entries(t, name, n):
 
 def _pages_of(page_table, batch):
     """Row length of a page table that has to have a row for each of `batch` requests."""
-    if page_table.dim() != 2 or page_table.size(0) < batch:
-        raise ValueError(f"page_table must be [>= {batch}, pages], got {tuple(page_table.shape)}")
-    return page_table.size(1)
+    shape = page_table.shape
+    if len(shape) != 2 or shape[0] < batch:
+        raise ValueError(f"page_table must be [>= {batch}, pages], got {tuple(shape)}")
+    return shape[1]
 
 
-def _rows_from(t, name, rows, heads, dtype):
-    """A [>= rows, heads, 128] tensor of that dtype."""
-    if t.dim() != 3 or t.size(0) < rows or t.size(1) != heads or t.size(2) != HEAD_DIM:
-        raise ValueError(f"{name} must be [>= {rows}, {heads}, {HEAD_DIM}], got {tuple(t.shape)}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+def _rows_from(t, name, rows, heads):
+    """Refuses what is not a [>= rows, heads, 128] tensor."""
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != HEAD_DIM:
+        raise ValueError(f"{name} must be [>= {rows}, {heads}, {HEAD_DIM}], got {tuple(shape)}")
+
+
+def _on(cache, here):
+    if here is not None and cache.device_index != here:
+        raise ValueError(f"the cache is on {cache.k.device}, but the current device is cuda:{here}")
 
 
 def append_kv4(token_indptr, total_tokens: int, max_tokens: int, k, v, page_table, ctx_len, cache: Kv4Cache,
@@ -572,38 +575,38 @@ def append_kv4(token_indptr, total_tokens: int, max_tokens: int, k, v, page_tabl
     bfloat16) behind every request's context and advance ctx_len (in place)."""
     code = _rows_code(k, "k", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v", total_tokens, cache.num_kv_heads, k.dtype)
-    _here(k, v, token_indptr, page_table, ctx_len, cache.k)
-    i32, batch = torch.int32, ctx_len.numel()
+    here, i32, batch = _here(), torch.int32, ctx_len.numel()
+    _on(cache, here)
     max_pages = _pages_of(page_table, batch)
     _entries(token_indptr, "token_indptr", batch + 1)
-    _check(_append_kv4(batch, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
-                       max_pages, max_ctx_len, _dev(token_indptr, "token_indptr", i32), total_tokens,
-                       max_tokens, _dev(k, "k"), _dev(v, "v"), _dev(page_table, "page_table", i32),
-                       _dev(ctx_len, "ctx_len", i32), cache.pointers, _stream(stream)), "d2sd_append_kv4")
+    _check(_append_kv4(batch, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages, max_pages, max_ctx_len,
+                       _dev(token_indptr, "token_indptr", i32, here), total_tokens, max_tokens, _dev(k, "k", None, here),
+                       _dev(v, "v", None, here), _dev(page_table, "page_table", i32, here),
+                       _dev(ctx_len, "ctx_len", i32, here), cache.pointers, _stream(stream)), "d2sd_append_kv4")
 
 
 def commit_accepted_kv4(B: int, node_indptr, total_nodes: int, path_nodes, accept_len, k_tree, v_tree, page_table,
                         ctx_len, cache: Kv4Cache, max_ctx_len: int, stream=None):
     """commit_accepted_kv for a 4-bit cache: the accepted rows are quantised as
     they are written (in place on the cache and on ctx_len)."""
-    code = _CODES.get(k_tree.dtype)
+    dt = k_tree.dtype
+    code = _CODES.get(dt)
     if code is None:
-        raise ValueError(f"k_tree dtype {k_tree.dtype} unsupported (float32 or bfloat16)")
-    _here(k_tree, v_tree, node_indptr, path_nodes, accept_len, page_table, ctx_len, cache.k)
-    _rows_from(k_tree, "k_tree", total_nodes, cache.num_kv_heads, k_tree.dtype)
-    _rows_from(v_tree, "v_tree", total_nodes, cache.num_kv_heads, k_tree.dtype)
-    i32, batch = torch.int32, ctx_len.numel()
+        raise ValueError(f"k_tree dtype {dt} unsupported (float32 or bfloat16)")
+    here, i32, batch = _here(), torch.int32, ctx_len.numel()
+    _on(cache, here)
+    k, v = _dev(k_tree, "k_tree", dt, here), _dev(v_tree, "v_tree", dt, here)
+    _rows_from(k_tree, "k_tree", total_nodes, cache.num_kv_heads)
+    _rows_from(v_tree, "v_tree", total_nodes, cache.num_kv_heads)
     max_pages = _pages_of(page_table, batch)
     _entries(node_indptr, "node_indptr", batch + 1)
-    _entries(path_nodes, "path_nodes", batch * B)
-    if batch > 1 and path_nodes.dim() == 2 and path_nodes.size(1) != B:
+    if path_nodes.numel() < batch * B or (batch > 1 and path_nodes.shape[-1] != B and path_nodes.dim() > 1):
         raise ValueError(f"path_nodes must be [{batch}, {B}], got {tuple(path_nodes.shape)}")
     _entries(accept_len, "accept_len", batch)
-    _check(_commit_kv4(batch, B, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
-                       max_pages, max_ctx_len, _dev(node_indptr, "node_indptr", i32), total_nodes,
-                       _dev(path_nodes, "path_nodes", i32), _dev(accept_len, "accept_len", i32),
-                       _dev(k_tree, "k_tree"), _dev(v_tree, "v_tree"), _dev(page_table, "page_table", i32),
-                       _dev(ctx_len, "ctx_len", i32), cache.pointers, _stream(stream)), "d2sd_commit_accepted_kv4")
+    _check(_commit_kv4(batch, B, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages, max_pages, max_ctx_len,
+                       _dev(node_indptr, "node_indptr", i32, here), total_nodes, _dev(path_nodes, "path_nodes", i32, here),
+                       _dev(accept_len, "accept_len", i32, here), k, v, _dev(page_table, "page_table", i32, here),
+                       _dev(ctx_len, "ctx_len", i32, here), cache.pointers, _stream(stream)), "d2sd_commit_accepted_kv4")
 
 
 def read_kv4(token_indptr, total_tokens: int, max_tokens: int, page_table, cache: Kv4Cache, start=None,
@@ -616,15 +619,15 @@ def read_kv4(token_indptr, total_tokens: int, max_tokens: int, page_table, cache
     v = v_out if v_out is not None else _empty_like(stream, k)
     code = _rows_code(k, "k_out", total_tokens, cache.num_kv_heads)
     _rows_code(v, "v_out", total_tokens, cache.num_kv_heads, k.dtype)
-    _here(k, v, token_indptr, start, page_table, cache.k)
-    i32, batch = torch.int32, token_indptr.numel() - 1
+    here, i32, batch = _here(), torch.int32, token_indptr.numel() - 1
+    _on(cache, here)
     max_pages = _pages_of(page_table, batch)
     if start is not None:
         _entries(start, "start", batch)
-    _check(_read_kv4(batch, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages,
-                     max_pages, _dev(token_indptr, "token_indptr", i32), total_tokens, max_tokens,
-                     _dev(start, "start", i32), _dev(page_table, "page_table", i32), cache.pointers, _dev(k, "k_out"),
-                     _dev(v, "v_out"), _stream(stream)), "d2sd_read_kv4")
+    _check(_read_kv4(batch, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, cache.num_pages, max_pages,
+                     _dev(token_indptr, "token_indptr", i32, here), total_tokens, max_tokens, _dev(start, "start", i32, here),
+                     _dev(page_table, "page_table", i32, here), cache.pointers, _dev(k, "k_out", None, here),
+                     _dev(v, "v_out", None, here), _stream(stream)), "d2sd_read_kv4")
     return k, v
 
 
@@ -636,25 +639,27 @@ def attn_args_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree, v_tree, node_
     code = _CODES.get(dt)
     if code is None:
         raise ValueError(f"q dtype {dt} unsupported (float32 or bfloat16)")
-    _here(q, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, out, lse, cache.k)
-    i32, batch, heads = torch.int32, ctx_len.numel(), q.size(1)
-    _rows_from(q, "q", total_nodes, heads, dt)
-    _rows_from(out, "out", total_nodes, heads, dt)
+    here, i32, batch = _here(), torch.int32, ctx_len.numel()
+    _on(cache, here)
+    heads = q.shape[1]
+    _rows_from(q, "q", total_nodes, heads)
+    _rows_from(out, "out", total_nodes, heads)
     if lse is not None:
         _entries(lse, "lse", total_nodes * heads)
     max_pages = _pages_of(page_table, batch)
     _entries(node_indptr, "node_indptr", batch + 1)
+    rows, words = anc_mask.shape if anc_mask is not None else (total_nodes, 0)
     if stage != STAGE_PREFIX:                          # which reads none of the tree's own
-        _rows_from(k_tree, "k_tree", total_nodes, cache.num_kv_heads, dt)
-        _rows_from(v_tree, "v_tree", total_nodes, cache.num_kv_heads, dt)
-        if anc_mask is not None and anc_mask.size(0) < total_nodes:
+        _rows_from(k_tree, "k_tree", total_nodes, cache.num_kv_heads)
+        _rows_from(v_tree, "v_tree", total_nodes, cache.num_kv_heads)
+        if rows < total_nodes:
             raise ValueError(f"anc_mask must be [>= {total_nodes}, words], got {tuple(anc_mask.shape)}")
-    a = AttnArgs(batch, heads, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, stage, sm_scale,
-                 total_nodes, max_nodes, max_ctx_len, cache.num_pages, max_pages,
-                 anc_mask.shape[1] if anc_mask is not None else 0, kv_split, 0, 0, _dev(q, "q", dt), None, None,
-                 _dev(page_table, "page_table", i32), _dev(ctx_len, "ctx_len", i32), _dev(k_tree, "k_tree", dt),
-                 _dev(v_tree, "v_tree", dt), _dev(node_indptr, "node_indptr", i32), _dev(anc_mask, "anc_mask", i32),
-                 _dev(out, "out", dt), _dev(lse, "lse", torch.float32), None)
+    a = AttnArgs(batch, heads, cache.num_kv_heads, HEAD_DIM, PAGE_SIZE, code, stage, sm_scale, total_nodes, max_nodes,
+                 max_ctx_len, cache.num_pages, max_pages, words, kv_split, 0, 0, _dev(q, "q", dt, here), None, None,
+                 _dev(page_table, "page_table", i32, here), _dev(ctx_len, "ctx_len", i32, here),
+                 _dev(k_tree, "k_tree", dt, here), _dev(v_tree, "v_tree", dt, here),
+                 _dev(node_indptr, "node_indptr", i32, here), _dev(anc_mask, "anc_mask", i32, here),
+                 _dev(out, "out", dt, here), _dev(lse, "lse", torch.float32, here), None)
     if node_indptr_host is not None:
         ip = _host_i32(node_indptr_host)
         if ip.shape != (a.batch + 1,):
@@ -683,13 +688,11 @@ def cascade_verify_attention_kv4(q, cache: Kv4Cache, page_table, ctx_len, k_tree
     a = attn_args_kv4(q, cache, page_table, ctx_len, k_tree, v_tree, node_indptr, anc_mask, out, lse,
                       total_nodes=total_nodes, max_nodes=max_nodes, max_ctx_len=max_ctx_len, stage=stage,
                       sm_scale=sm_scale, kv_split=kv_split, node_indptr_host=node_indptr_host)
-    if workspace is None:      # a given one's size is checked against the call's need by the library
+    if workspace is None:      # a given one is checked against the call's need by the library
         need = cascade_workspace_size_kv4(a)
         if need > 0:
             workspace = _empty(stream, need, torch.uint8, q.device)
-    else:
-        _here(workspace)
-    ws_ptr = _dev(workspace, "workspace") if workspace is not None else None
+    ws_ptr = _dev(workspace, "workspace", None, _here()) if workspace is not None else None
     ws_len = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(_cascade_kv4(ctypes.byref(a), cache.pointers, ws_ptr, ws_len, _stream(stream)),
            "d2sd_cascade_verify_attention_kv4")
@@ -714,9 +717,9 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
         raise ValueError(f"logits dtype {logits.dtype} unsupported (float32 or bfloat16)")
     if logits.dim() != 2 or logits.shape[0] < total_nodes:
         raise ValueError(f"logits must be [>= {total_nodes}, vocab], got {tuple(logits.shape)}")
-    _here(logits, node_indptr, depth, anc_mask, draft_tokens, history, history_len, prompt_len, repetition, presence, frequency,
-          bias_token, bias_value, bias_len, token_mask, mask_row, out)
     batch, vocab = node_indptr.numel() - 1, logits.shape[1]
+    here = _here()
+    x = _dev(logits, "logits", None, here)
     if out is None:
         out = _empty_like(stream, logits)
     if out.shape != logits.shape:
@@ -739,14 +742,14 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
     i32, f32 = torch.int32, torch.float32
     a = LogitsArgs(batch, total_nodes, max_nodes, anc_mask.shape[1], vocab, code,
                    history.shape[1] if history is not None else 0, bias_token.shape[1] if bias_token is not None else 0,
-                   token_mask.shape[0] if token_mask is not None else 0, _dev(node_indptr, "node_indptr", i32),
-                   _dev(depth, "depth", i32), _dev(anc_mask, "anc_mask", i32), _dev(draft_tokens, "draft_tokens", i32),
-                   _dev(logits, "logits"), _dev(history, "history", i32), _dev(history_len, "history_len", i32),
-                   _dev(prompt_len, "prompt_len", i32), _dev(repetition, "repetition", f32),
-                   _dev(presence, "presence", f32), _dev(frequency, "frequency", f32),
-                   _dev(bias_token, "bias_token", i32), _dev(bias_value, "bias_value", f32),
-                   _dev(bias_len, "bias_len", i32), _dev(token_mask, "token_mask", i32),
-                   _dev(mask_row, "mask_row", i32), _dev(out, "out", logits.dtype))
+                   token_mask.shape[0] if token_mask is not None else 0, _dev(node_indptr, "node_indptr", i32, here),
+                   _dev(depth, "depth", i32, here), _dev(anc_mask, "anc_mask", i32, here), _dev(draft_tokens, "draft_tokens", i32, here),
+                   x, _dev(history, "history", i32, here), _dev(history_len, "history_len", i32, here),
+                   _dev(prompt_len, "prompt_len", i32, here), _dev(repetition, "repetition", f32, here),
+                   _dev(presence, "presence", f32, here), _dev(frequency, "frequency", f32, here),
+                   _dev(bias_token, "bias_token", i32, here), _dev(bias_value, "bias_value", f32, here),
+                   _dev(bias_len, "bias_len", i32, here), _dev(token_mask, "token_mask", i32, here),
+                   _dev(mask_row, "mask_row", i32, here), _dev(out, "out", logits.dtype, here))
     _check(_adjust(ctypes.byref(a), _stream(stream)), "d2sd_adjust_logits")
     return out
 
