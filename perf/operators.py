@@ -338,9 +338,9 @@ def _own_pass(s):
             history_len=s["history_len"], prompt_len=s["prompt_len"], repetition=s["repetition"], presence=s["presence"],
             frequency=s["frequency"], bias_token=s.get("bias_token"), bias_value=s.get("bias_value"), bias_len=s.get("bias_len"),
             token_mask=s.get("token_mask"), mask_row=s.get("mask_row"))
-    if "cache" not in s:
-        s["cache"] = d2sd.Kv4Cache(s["k"], s["v"], s["k_scale"], s["v_scale"])
-    cache = s["cache"]
+    cache = s.get("cache")
+    if cache is None or cache.k is not s["k"] or cache.v is not s["v"] or cache.k_scale is not s["k_scale"] or cache.v_scale is not s["v_scale"]:
+        cache = s["cache"] = d2sd.Kv4Cache(s["k"], s["v"], s["k_scale"], s["v_scale"])
     if kind == "attn":
         if "out" not in s:  # the buffers that a serving loop keeps
             s["out"], s["lse"] = torch.empty_like(s["q"]), torch.empty(s["q"].shape[:2], device=DEV)
@@ -352,13 +352,16 @@ def _own_pass(s):
             s["q"], cache, s["table"], s["ctx"], s["k_tree"], s["v_tree"], s["ip"], s["mask"], total_nodes=s["total"],
             max_nodes=s["max_nodes"], max_ctx_len=s["max_ctx"], node_indptr_host=s["ip_host"], out=s["out"], lse=s["lse"], workspace=s["ws"])
         return {"out": s["out"], "lse": s["lse"]}
+    ctx = s["ctx"]
+    if kind != "read":  # every pass writes behind the same contexts, whose lengths the call advances
+        ctx = s["start"].clone()
     if kind == "append":
-        d2sd.append_kv4(s["tip"], s["tokens"], s["max_tokens"], s["k_new"], s["v_new"], s["table"], s["ctx"], cache, s["max_ctx"])
+        d2sd.append_kv4(s["tip"], s["tokens"], s["max_tokens"], s["k_new"], s["v_new"], s["table"], ctx, cache, s["max_ctx"])
     if kind == "commit":
         d2sd.commit_accepted_kv4(s["B"], s["ip"], s["total"], s["path_nodes"], s["accept_len"], s["k_new"], s["v_new"],
-                                 s["table"], s["ctx"], cache, s["max_ctx"])
+                                 s["table"], ctx, cache, s["max_ctx"])
     k, v = d2sd.read_kv4(s["tip"], s["tokens"], s["max_tokens"], s["table"], cache, start=s["start"], dtype=s["dtype"])
-    return {"k": k, "v": v} if kind == "read" else {"k": k, "v": v, "ctx": s["ctx"]}
+    return {"k": k, "v": v} if kind == "read" else {"k": k, "v": v, "ctx": ctx}
 
 
 def run(s):
