@@ -609,7 +609,7 @@ d2sd_status d2sd_cascade_verify_attention_kv4(const d2sd_attn_args* args, const 
  *   x     = logits[n, j];
  *   x     = x > 0 ? x / repetition[b] : x * repetition[b]     if seen;
  *   x     = x - count * frequency[b] - (count > 0) * presence[b];
- *   x     = x + the bias values of j in the request's list, in list order;
+ *   x     = x + the sum of j's bias values in the request's list, taken in list order;
  *   x     = -inf   if mask_row[n] >= 0 and bit j of token_mask[mask_row[n]] is 0.
  * Evaluated in fp32 and rounded once to dtype. Lists and masks that are NULL
  * are left out. Token ids outside [0, vocab) are ignored, lengths are clamped
@@ -647,7 +647,10 @@ typedef struct d2sd_logits_args {
 /*
  * Device. Adjusts the logits of every tree node (see d2sd_logits_args) for
  * d2sd_sample_targets or an argmax. A row whose mask leaves nothing is all
- * -inf, for which d2sd_sample_targets gives -1. One launch, no workspace.
+ * -inf, for which d2sd_sample_targets gives -1. One launch, no workspace. A
+ * request's history and bias list are read once per 2048 tokens of the vocabulary
+ * and up to eight of its nodes: of 32000 logits, 4000 tokens of history add 7% to
+ * the time, 32000 add 45%.
  * Errors: INVALID_ARG, or UNSUPPORTED from 2^24 of batch * max_nodes *
  * ceil(vocab / 2048) on, before any launch.
  */

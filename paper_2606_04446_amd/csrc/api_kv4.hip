@@ -75,14 +75,14 @@ constexpr long long kMaxUnits = 1ll << 24;              // of one request's stre
 // Two workgroups of four waves per CU are resident (bf16; one with fp32, whose
 // terms take twice the registers), and that is the grid unless a share would
 // fall below kMinSteps steps of keys, less than which is not worth a partial
-// state (one request of one token over 4096 keys: 21.1 us with two, 21.9 with
-// one, 23.8 with three).
+// state (one request of one token over 4096 keys: 18.5 us with two, 21.5 with
+// one, 20.0 with three).
 //
 // A stream's start, tree and end take as long as some steps of its keys, 10 to
 // 15 us, and a share that holds many short streams would end last. They are
 // charged kCharge units of cost (a step of four row tiles is 8), at most a
-// share: 64 requests of one token over 500 to 16000 keys took 181 us with 3,
-// 167 with 10, 150 with 20, 129 with 30 and 132 with 45.
+// share: 64 requests of one token over 500 to 16000 keys take 178 us with 3,
+// 164 with 10, 146 with 20, 130 with 30 and 132 with 45.
 constexpr int kMinSteps = 2;
 constexpr long long kCharge = 30;
 
@@ -91,10 +91,10 @@ constexpr long long kCharge = 30;
 // longest stream's steps; cut, a start and one more per stream of a share, the
 // share (contexts of three quarters of the largest) and the merge, whose states
 // grow with the rows. fp32 steps count for a quarter more. us cut, uncut: 64
-// requests of one token over 100 to 2000 keys 45, 32 (over 500 to 16000 the
-// longest stream alone takes 165, all shares 129); 24 over 100 to 1000 27, 20; 16
-// of six row tiles over 500 keys 42, 27, 32 over 1000 70, 51, 64 over 100 to 500
-// 92, 74; fp32, 6 of one token and two KV heads over 706 keys 20, 28.
+// requests of one token over 100 to 2000 keys 46, 33 (over 500 to 16000 130,
+// 150); 24 over 100 to 1000 28, 21; 16 of up to eight row tiles over 500 keys 42,
+// 28, 32 over 1000 73, 53, 64 over 100 to 500 95, 75; fp32, 6 of one token and two
+// KV heads over 706 keys 20.5, 28.
 bool whole_pays(bool bf16, long long streams, long long resident, long long steps, long long cost, int most, int grid) {
   const double step = bf16 ? 1.0 : 1.25;
   const double uncut = fmax(1.0, (double)streams / resident) * (kCharge + step * steps * most);

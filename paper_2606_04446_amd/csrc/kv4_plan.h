@@ -21,8 +21,8 @@ struct Kv4Plan {
 // Cost of a step (128 keys) for a workgroup that holds 1, 2 or 4 row tiles, and
 // of a step for all `tiles` row tiles of a KV head (four at a time, then two,
 // then one). The matrix cores' part is proportional to the tiles, that of copies
-// and barriers is not; 32 requests of 16384 keys and up to 14 tiles take 847 us
-// with 8 : 5 : 3, 855 with 8 : 4 : 2 and 855 with 18 : 9 : 5.
+// and barriers is not; 32 requests of 16384 keys and up to 14 tiles take 863 us
+// with 8 : 5 : 3, 872 with 8 : 4 : 2 and 874 with 18 : 9 : 5.
 __host__ __device__ inline int kv4_cost(int tiles) { return 8 * (tiles >> 2) + (tiles & 2 ? 5 : 0) + (tiles & 1 ? 3 : 0); }
 
 hipError_t launch_kv4_attention(const d2sd_attn_args& a, const d2sd_kv4_cache& cache, const Kv4Plan& plan, void* ws,
