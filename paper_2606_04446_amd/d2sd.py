@@ -718,6 +718,7 @@ def adjust_logits(node_indptr, total_nodes: int, max_nodes: int, depth, anc_mask
     if logits.dim() != 2 or logits.shape[0] < total_nodes:
         raise ValueError(f"logits must be [>= {total_nodes}, vocab], got {tuple(logits.shape)}")
     batch, vocab = node_indptr.numel() - 1, logits.shape[1]
+    _dev(logits, "logits")                             # a host tensor, before the device is asked for
     here = _here()
     x = _dev(logits, "logits", None, here)
     if out is None:

@@ -232,3 +232,12 @@ def test_adjust_refuses_short_tensors(calls, kw, what):
     with pytest.raises(ValueError, match=what):
         adjust(**kw)
     assert not calls
+
+
+def test_adjust_refuses_host_tensors_where_there_is_no_device(monkeypatch):
+    def none():
+        raise RuntimeError("no device")
+    monkeypatch.setattr(d2sd, "_current_device", none)
+    i = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="logits must be a device tensor"):
+        d2sd.adjust_logits(i, 1, 1, i, torch.zeros((1, 1), dtype=torch.int32), i, torch.zeros((1, 8)))
