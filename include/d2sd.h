@@ -588,7 +588,8 @@ d2sd_status d2sd_cascade_workspace_size_kv4(const d2sd_attn_args* args, size_t* 
  * in 24 bits in fp32 ones. Results do not depend on what else runs, nor on the
  * workspace's contents, and nothing is kept in it.
  * A tree value that is infinite or NaN reaches the rows that see its node and
- * no other. A row that sees no key gets out = 0, lse = -inf. Errors: as there;
+ * no other; so does a tree key, which in fp32 makes these rows NaN whatever the
+ * sign of its scores. A row that sees no key gets out = 0, lse = -inf. Errors: as there;
  * UNSUPPORTED also above about 2^28 of (max_ctx_len / 128 + max_nodes / 64 +
  * 18) * max_nodes * num_qo_heads (250000 tokens of context with 2080 nodes and
  * 64 query heads).
