@@ -57,3 +57,30 @@ def test_a_largest_key_takes_all_or_nothing(value, kv_split):
     b.mask = dev(mask_of([Rows(without)], b.W))
     ref, ref_lse = b.run(kv_split=kv_split)
     assert torch.equal(out[:, 1], ref[:, 1]) and torch.equal(lse[:, 1], ref_lse[:, 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf")])
+def test_an_infinite_key_stays_with_the_rows_that_see_it(value, dtype):
+    """Rows that see it are NaN in fp32; in bf16 where its score is +inf, and without the node where it is -inf."""
+    trees = canonical(16, [[3, 9]])
+    b = Batch(trees, [100], 4, 2, dtype, seed=73)
+    vis, node = trees[0].visible(), trees[0].N - 1
+    b.q[:, 0, 5], b.q[:, 1, 5] = 0.5, -0.5
+    ref, ref_lse = (t.clone() for t in b.run())
+    b.kt[node, 0, 5] = value
+    out, lse = b.run()
+    sees, unseen = np.flatnonzero(vis[:, node]), np.flatnonzero(~vis[:, node])
+    assert torch.equal(out[unseen], ref[unseen]) and torch.equal(lse[unseen], ref_lse[unseen])
+    assert torch.equal(out[:, 2:], ref[:, 2:]) and torch.equal(lse[:, 2:], ref_lse[:, 2:])
+    up = 0 if value > 0 else 1                          # the head whose score is +inf
+    assert out[sees, up].isnan().all()
+    if dtype == "f32":
+        assert out[sees, 1 - up].isnan().all() and lse[sees, 1 - up].isnan().all()
+        return
+    without = vis.copy()
+    without[:, node] = False
+    b.kt[node, 0, 5] = 0.0
+    b.mask = dev(mask_of([Rows(without)], b.W))
+    ref, ref_lse = b.run()
+    assert torch.equal(out[:, 1 - up], ref[:, 1 - up]) and torch.equal(lse[:, 1 - up], ref_lse[:, 1 - up])
